@@ -271,6 +271,98 @@ int qat_adam_step(float *param, const float *grad, float *m, float *v, int64_t c
 int qat_sgd_step(float *param, const float *grad, int64_t count, float lr, float grad_clip,
                  hipStream_t stream);
 
+/* ---------------------------------------------------------------------
+ * The quantised linear layer: what trains and answers with the codewords.
+ *
+ * Types and activations.  dtype is the type of x, W, bias, residual, y, their
+ * gradients and of the matrix instructions' operands; every sum is held in
+ * fp32.  Matrices are row-major with a leading dimension in elements (ldx >=
+ * columns); pointers are aligned to their element, codes to 16 bytes.  Inputs
+ * and outputs must not overlap.  Rows up to 2^31 - 1, columns up to 2^22 - 1,
+ * else BCJR_ERR_UNSUPPORTED.  Every call gives the same bits each time. */
+#define QAT_F32 0
+#define QAT_BF16 1
+#define QAT_F16 2
+#define QAT_ACT_NONE 0
+#define QAT_ACT_SILU 1       /* z / (1 + exp(-z)) */
+#define QAT_ACT_GELU 2       /* z Phi(z) */
+#define QAT_ACT_GELU_TANH 3  /* its tanh form */
+
+/* 8-bit checkpoints of an activation x [rows, cols].  A group is 32 rows of
+ * one column, rows 32 g .. 32 g + 31; with 2^e the smallest power of two for
+ * which amax <= 127 * 2^e (e >= -126, for fp16 e >= -24), value v is held as
+ *     q = round-half-even(v / 2^e)
+ * (|q| <= 63 at e = 122, for fp16 at e = 10, where 64 would overflow the
+ * type) and read back as q * 2^e: at most half a step 2^e off, exact in the
+ * type.  codes is [ceil(rows / 32), cols, 32] int8, the last group's missing
+ * rows 0; scales is [ceil(rows / 32), cols], the bf16 bits of 2^e.  A
+ * non-finite value is held as -128, reads back as NaN, does not count towards
+ * amax, and makes its group's scale negative. */
+int qat_act8_store(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t *codes,
+                   uint16_t *scales, hipStream_t stream);
+int qat_act8_load(const int8_t *codes, const uint16_t *scales, int64_t rows, int64_t cols, void *out,
+                  int dtype, int64_t ldo, hipStream_t stream);
+
+/* y = activation(z) + residual, z = x W^T + bias, for x [M, K], W [N, K],
+ * bias [N] or NULL, residual [M, N] or NULL, y [M, N].  z_codes and z_scales
+ * (both or neither) receive the 8-bit checkpoint of z, taken from the fp32
+ * sums (as for dtype QAT_F32).  M == 0 is a no-op.  Workspace:
+ * qat_linear_act_workspace_bytes() bytes, 16-byte aligned (NULL where 0). */
+size_t qat_linear_act_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K);
+int qat_linear_act(const void *x, int64_t ldx, const void *W, int64_t ldw, const void *bias,
+                   const void *residual, int64_t ldr, int dtype, int activation, int64_t M, int64_t N,
+                   int64_t K, void *y, int64_t ldy, int8_t *z_codes, uint16_t *z_scales,
+                   void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Its backward pass from 8-bit checkpoints: for the upstream gradient dy [M, N]
+ *     dz = dy * activation'(z),  dx = dz W,  dW = dz^T x,  dbias = sum_m dz
+ * with z [M, N] and x [M, K] read from their checkpoints (z is unused for
+ * QAT_ACT_NONE).  dx [M, K], dW [N, K] and dbias [N] are dense; NULL where
+ * unwanted, and then W (dx) and x (dW) may be NULL too.  dz is rounded to
+ * dtype once, as the operand of the two products; dbias sums it unrounded.
+ * The residual's gradient is dy itself.  x must have been stored in dtype.  A
+ * group of x that holds a non-finite value makes its column of dW NaN.
+ * M == 0 gives zero dW and dbias. */
+size_t qat_linear_act_vjp_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K, int activation);
+int qat_linear_act_vjp(const void *dy, int64_t ldd, const int8_t *x_codes, const uint16_t *x_scales,
+                       const void *W, int64_t ldw, const int8_t *z_codes, const uint16_t *z_scales,
+                       int dtype, int activation, int64_t M, int64_t N, int64_t K, void *dx, void *dW,
+                       void *dbias, void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Trellis paths as bit strings.  A path of `steps` states is the n =
+ * state_bits bits of its first state and then the k new bits of each further
+ * one, most significant bit first, in 32-bit words: bit p of the string is bit
+ * 31 - p % 32 of word p / 32, and the state after step t is the n-bit window
+ * at bit t k.  A path takes trellis_words() = ceil((n + (steps - 1) k) / 32)
+ * words for block = steps * V weights (0 for invalid arguments); what is left
+ * of the last word is written 0 and not read.  steps <= 2^24.
+ * trellis_pack writes packed [B, words] from states [B, steps]; illegal, if
+ * given, receives the number of states outside 0 .. 2^n - 1 or not reachable
+ * from the one before (the strings are then meaningless). */
+int64_t trellis_words(int state_bits, int k, int V, int64_t block);
+int trellis_pack(const int32_t *states, int64_t B, int64_t steps, int state_bits, int k,
+                 uint32_t *packed, int32_t *illegal, hipStream_t stream);
+int trellis_unpack(const uint32_t *packed, int64_t B, int64_t steps, int state_bits, int k,
+                   int32_t *states, hipStream_t stream);
+
+/* The codewords of B paths, times scales [B] if given: W [B, block] of type
+ * dtype, from codebook [S] (V = 1) or [S, V] in fp32, 1 <= V <= 8. */
+int trellis_dense(const uint32_t *packed, int64_t B, const float *codebook, int state_bits, int k, int V,
+                  int64_t block, const float *scales, void *W, int dtype, hipStream_t stream);
+
+/* qat_linear_act with W [N, K] given by its paths: packed [N, K / block,
+ * words], row n's weights block by block, times scales [N, K / block] if
+ * given.  K must be a multiple of block.  The weights are rounded to dtype
+ * (before or after their scale) as the matrix instructions' operands.
+ * Workspace: trellis_linear_workspace_bytes() bytes, 16-byte aligned. */
+size_t trellis_linear_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K, int state_bits, int k,
+                                      int V, int64_t block);
+int trellis_linear(const void *x, int64_t ldx, const uint32_t *packed, const float *codebook,
+                   int state_bits, int k, int V, int64_t block, const float *scales, const void *bias,
+                   const void *residual, int64_t ldr, int dtype, int activation, int64_t M, int64_t N,
+                   int64_t K, void *y, int64_t ldy, void *workspace, size_t ws_bytes,
+                   hipStream_t stream);
+
 /* Static description of a status code; never NULL. */
 const char *bcjr_status_string(int status);
 

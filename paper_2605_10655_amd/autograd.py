@@ -1,4 +1,5 @@
-"""Autograd node of the soft codeword (Sec. 3.5) and its BCJR-STE variant.
+"""Autograd nodes: the soft codeword (Sec. 3.5) with its BCJR-STE variant, and
+the linear layer that multiplies activations with it.
 
 ``BcjrQuant`` wraps the library's entry points as a ``torch.autograd.Function``:
 
@@ -12,14 +13,21 @@
 T is a plain number read at call time (a detached schedule value, Sec. 3.5),
 so it gets no gradient.  Gradients flow to the weights and, if it requires
 grad, to the codebook.  Every step runs in the library's HIP kernels.
+
+``LinearAct8`` is activation(x W^T + bias) + residual whose backward pass reads
+x and z = x W^T + bias from 8-bit checkpoints (``linear.Act8``) in place of the
+activations themselves: 2.1 bytes a value pair are kept instead of 4 (bf16) or
+8 (fp32).  dW is taken with the checkpoint's x, the activation's derivative at
+the checkpoint's z; everything else is exact up to rounding.
 """
 from __future__ import annotations
 
 import torch
 
 from . import bcjr_soft_codeword, bcjr_soft_codeword_vjp, bcjr_ste_vjp, viterbi_decode
+from .linear import Act8, act8_store, linear_act, linear_act_vjp
 
-__all__ = ["BcjrQuant", "bcjr_quant"]
+__all__ = ["BcjrQuant", "bcjr_quant", "LinearAct8", "linear_act8"]
 
 
 def _temperature(T) -> float:
@@ -72,3 +80,47 @@ def bcjr_quant(W, codebook, state_bits: int, k: int, T, block: int = 256, hard: 
         raise ValueError(f"W.numel() = {W.numel()} is not a multiple of block = {block}")
     out = BcjrQuant.apply(W.reshape(-1, block), codebook, state_bits, k, T, hard)
     return out.reshape(W.shape)
+
+
+class LinearAct8(torch.autograd.Function):
+    """activation(x W^T + bias) + residual with 8-bit checkpoints."""
+
+    @staticmethod
+    def forward(ctx, x, W, bias, residual, activation, x8):
+        need_x, need_W, need_b, need_r = ctx.needs_input_grad[:4]
+        need_z = activation != "none" and (need_x or need_W or need_b)
+        out = linear_act(x, W, bias, residual, activation, save=need_z)
+        y, z8 = out if need_z else (out, None)
+        if need_W and x8 is None:
+            x8 = act8_store(x)
+        ctx.activation, ctx.x_shape = activation, x.shape
+        ctx.rows, ctx.cols, ctx.dtype = x.numel() // max(x.shape[-1], 1), x.shape[-1], x.dtype
+        ctx.save_for_backward(W if need_x else None, *((x8.codes, x8.scales) if need_W else (None, None)),
+                              *((z8.codes, z8.scales) if need_z else (None, None)))
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        need_x, need_W, need_b, need_r = ctx.needs_input_grad[:4]
+        W, xc, xs, zc, zs = ctx.saved_tensors
+        g = dy.contiguous()
+        x8 = Act8(xc, xs, ctx.rows, ctx.dtype) if need_W else None
+        z8 = Act8(zc, zs, ctx.rows, torch.float32) if zc is not None else None
+        dx, dW, db = linear_act_vjp(g, x8, W, z8, ctx.activation if z8 is not None else "none",
+                                    want_dx=need_x, want_dW=need_W, want_dbias=need_b)
+        return dx, dW, db, dy if need_r else None, None, None
+
+
+def linear_act8(x, W, bias=None, residual=None, activation="none", x8=None):
+    """activation(x W^T + bias) + residual, x [..., K], W [N, K] (float32,
+    bfloat16 or float16, one type for all), differentiable in all four; the
+    backward pass reads x and x W^T + bias in 8 bits.  x8: the checkpoint
+    act8_store(x), where several layers read the same x."""
+    if x8 is not None:
+        if not isinstance(x8, Act8):
+            raise TypeError("x8 must be an Act8")
+        rows = x.numel() // max(x.shape[-1], 1)
+        if (x8.rows, x8.cols, x8.dtype) != (rows, x.shape[-1], x.dtype):
+            raise ValueError("x8 is not a checkpoint of x: its size or type differs")
+    return LinearAct8.apply(x, W, bias, residual, activation, x8)

@@ -2,12 +2,12 @@
 C ABI of include/bcjr.h) and libissue_rates.so (the VALU issue-rate probe
 the benchmark prices its roofline with).
 
-libbcjr.so links three translation units, compiled side by side:
+libbcjr.so links four translation units, compiled side by side:
 bcjr_capi.hip (the C ABI and most kernel families), bcjr_rot.hip (the
 rotating-exchange kernels of S = 65536, k = 2), which is compiled with the
-AMDGPU max-ilp instruction scheduler, and bcjr_lin.hip (the linear-domain
-kernels of the smaller trellises); each object carries its own code
-object."""
+AMDGPU max-ilp instruction scheduler, bcjr_lin.hip (the linear-domain
+kernels of the smaller trellises) and qat_linear.hip (the quantised linear
+layer); each object carries its own code object."""
 from __future__ import annotations
 
 import os
@@ -25,14 +25,15 @@ LIB = os.path.join(PKG, "libbcjr.so")
 # (source, extra compiler flags)
 UNITS = [(os.path.join(CSRC, "bcjr_capi.hip"), []),
          (os.path.join(CSRC, "bcjr_rot.hip"), ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]),
-         (os.path.join(CSRC, "bcjr_lin.hip"), [])]
+         (os.path.join(CSRC, "bcjr_lin.hip"), []),
+         (os.path.join(CSRC, "qat_linear.hip"), [])]
 SOURCES = [u[0] for u in UNITS]
 RATES_SRC = os.path.join(CSRC, "issue_rates.hip")
 RATES_LIB = os.path.join(PKG, "libissue_rates.so")
 DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in (
     "bcjr_device.h", "bcjr_kernels.h", "bcjr_vec_kernels.h", "bcjr_qat.h", "bcjr_internal.h",
     "bcjr_generic_kernels.h", "bcjr_ldlq_kernels.h", "bcjr_rot_kernels.h", "bcjr_pruned_kernels.h",
-    "bcjr_lin_kernels.h")] + [
+    "bcjr_lin_kernels.h", "qat_linear_kernels.h")] + [
     os.path.join(INCLUDE, "bcjr.h")]
 
 BASE_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,302 @@
+// qat_linear.hip -- C ABI of the quantised linear layer (declared in
+// include/bcjr.h): argument checks, choice of kernels, workspace carving and
+// launches.  Its own translation unit.
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "bcjr.h"
+#include "qat_linear_kernels.h"
+
+namespace bcjr {
+namespace qlin {
+namespace {
+
+constexpr size_t kAlign = 256;
+size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Limits of the grids: columns of any operand lie along a grid's second axis.
+constexpr int64_t kMaxRows = (int64_t)1 << 31, kMaxCols = (int64_t)1 << 22;
+
+int elem_size(int dtype) { return dtype == kF32 ? 4 : 2; }
+bool dtype_ok(int dtype) { return dtype == kF32 || dtype == kBF16 || dtype == kF16; }
+bool act_ok(int act) { return act >= kActNone && act <= kActGeluTanh; }
+bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+bool dims_ok(int64_t M, int64_t N, int64_t K) { return M >= 0 && N >= 1 && K >= 1; }
+bool dims_fit(int64_t M, int64_t N, int64_t K) { return M < kMaxRows && N < kMaxCols && K < kMaxCols; }
+int launched() { return hipGetLastError() == hipSuccess ? BCJR_OK : BCJR_ERR_HIP; }
+
+template <class F>
+int by_type(int dtype, F f) {
+  if (dtype == kBF16) return f(bf16());
+  if (dtype == kF16) return f(f16());
+  return f(float());
+}
+
+dim3 group_grid(int64_t rows, int64_t cols, int threads) {
+  return dim3((unsigned)ceil_div(rows, kRows), (unsigned)ceil_div(cols, threads));
+}
+
+template <class T, int AM, int BM>
+int gemm(const GemmArgs& g, hipStream_t stream) {
+  if (g.I == 0 || g.J == 0) return BCJR_OK;
+  hipLaunchKernelGGL((gemm_kernel<T, AM, BM>), dim3((unsigned)ceil_div(g.I, kTile), (unsigned)ceil_div(g.J, kTile)),
+                     dim3(256), 0, stream, g);
+  return launched();
+}
+
+int run_linear(const GemmArgs& g, int dtype, hipStream_t stream) {
+  return by_type(dtype, [&](auto t) -> int { return gemm<decltype(t), kRow, kRow>(g, stream); });
+}
+
+struct VjpPlan {
+  size_t dz, part, total;
+};
+
+VjpPlan vjp_plan(int dtype, int64_t M, int64_t N, int act) {
+  VjpPlan p;
+  p.dz = act == kActNone ? 0 : align_up((size_t)(M * N) * elem_size(dtype));
+  p.part = align_up((size_t)(ceil_div(M, kRows) * N) * sizeof(float));
+  p.total = p.dz + p.part;
+  return p;
+}
+
+struct Code {
+  int n, k, V;
+  int64_t block, steps, words;
+};
+
+// false where the arguments name no trellis
+bool code_of(int state_bits, int k, int V, int64_t block, Code* c) {
+  if (k < 1 || state_bits < k || state_bits > 16 || V < 1 || V > 8 || block < 1 || block % V || block > (1 << 24))
+    return false;
+  c->n = state_bits;
+  c->k = k;
+  c->V = V;
+  c->block = block;
+  c->steps = block / V;
+  c->words = ceil_div(state_bits + (c->steps - 1) * k, 32);
+  return true;
+}
+
+template <class T>
+int run_dense(const uint32_t* packed, const float* codebook, const float* scales, const Code& c, int64_t B, T* W,
+              hipStream_t stream) {
+  hipLaunchKernelGGL(dense_kernel<T>, dim3((unsigned)ceil_div(B * c.steps, 256)), dim3(256), 0, stream, packed,
+                     codebook, scales, B, c.steps, c.n, c.k, c.V, c.words, W);
+  return launched();
+}
+
+// blocks of 256 threads that one launch can have
+bool threads_fit(int64_t n) { return ceil_div(n, 256) < ((int64_t)1 << 31); }
+
+}  // namespace
+}  // namespace qlin
+}  // namespace bcjr
+
+using namespace bcjr::qlin;
+
+extern "C" {
+
+int qat_act8_store(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t* codes,
+                   uint16_t* scales, hipStream_t stream) {
+  if (!dtype_ok(dtype) || rows < 0 || cols < 1 || ldx < cols) return BCJR_ERR_INVALID_ARG;
+  if (rows >= kMaxRows || cols >= kMaxCols) return BCJR_ERR_UNSUPPORTED;
+  if (rows == 0) return BCJR_OK;
+  if (!x || !codes || !scales || misaligned(x, elem_size(dtype)) || misaligned(codes, 16) || misaligned(scales, 2))
+    return BCJR_ERR_INVALID_ARG;
+  return by_type(dtype, [&](auto t) -> int {
+    using T = decltype(t);
+    hipLaunchKernelGGL(act8_store_kernel<T>, group_grid(rows, cols, 64), dim3(64), 0, stream,
+                       static_cast<const T*>(x), rows, cols, ldx, codes, scales);
+    return launched();
+  });
+}
+
+int qat_act8_load(const int8_t* codes, const uint16_t* scales, int64_t rows, int64_t cols, void* out, int dtype,
+                  int64_t ldo, hipStream_t stream) {
+  if (!dtype_ok(dtype) || rows < 0 || cols < 1 || ldo < cols) return BCJR_ERR_INVALID_ARG;
+  if (rows >= kMaxRows || cols >= kMaxCols) return BCJR_ERR_UNSUPPORTED;
+  if (rows == 0) return BCJR_OK;
+  if (!out || !codes || !scales || misaligned(out, elem_size(dtype)) || misaligned(codes, 16) ||
+      misaligned(scales, 2))
+    return BCJR_ERR_INVALID_ARG;
+  return by_type(dtype, [&](auto t) -> int {
+    using T = decltype(t);
+    hipLaunchKernelGGL(act8_load_kernel<T>, group_grid(rows, cols, 64), dim3(64), 0, stream, codes, scales, rows,
+                       cols, static_cast<T*>(out), ldo);
+    return launched();
+  });
+}
+
+size_t qat_linear_act_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K) {
+  (void)dtype, (void)M, (void)N, (void)K;
+  return 0;
+}
+
+int qat_linear_act(const void* x, int64_t ldx, const void* W, int64_t ldw, const void* bias, const void* residual,
+                   int64_t ldr, int dtype, int activation, int64_t M, int64_t N, int64_t K, void* y, int64_t ldy,
+                   int8_t* z_codes, uint16_t* z_scales, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || ldx < K || ldw < K || ldy < N ||
+      (residual && ldr < N) || (!z_codes != !z_scales))
+    return BCJR_ERR_INVALID_ARG;
+  if (!dims_fit(M, N, K)) return BCJR_ERR_UNSUPPORTED;
+  if (M == 0) return BCJR_OK;
+  const size_t es = elem_size(dtype);
+  if (!x || !W || !y || misaligned(x, es) || misaligned(W, es) || misaligned(y, es) || misaligned(bias, es) ||
+      misaligned(residual, es) || misaligned(z_codes, 16) || misaligned(z_scales, 2))
+    return BCJR_ERR_INVALID_ARG;
+  const size_t need = qat_linear_act_workspace_bytes(dtype, M, N, K);
+  if (need && (!workspace || misaligned(workspace, 16) || ws_bytes < need)) return BCJR_ERR_WORKSPACE;
+  const GemmArgs g = {x, W, ldx, ldw, nullptr, M, N, K, bias, residual, ldr, y, ldy, z_codes, z_scales, activation};
+  return run_linear(g, dtype, stream);
+}
+
+size_t qat_linear_act_vjp_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K, int activation) {
+  if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || !dims_fit(M, N, K)) return 0;
+  return vjp_plan(dtype, M, N, activation).total;
+}
+
+int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const uint16_t* x_scales, const void* W,
+                       int64_t ldw, const int8_t* z_codes, const uint16_t* z_scales, int dtype, int activation,
+                       int64_t M, int64_t N, int64_t K, void* dx, void* dW, void* dbias, void* workspace,
+                       size_t ws_bytes, hipStream_t stream) {
+  if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || ldd < N || (dx && ldw < K))
+    return BCJR_ERR_INVALID_ARG;
+  if (!dims_fit(M, N, K)) return BCJR_ERR_UNSUPPORTED;
+  if (!dx && !dW && !dbias) return BCJR_OK;
+  const size_t es = elem_size(dtype);
+  if (misaligned(dy, es) || misaligned(W, es) || misaligned(dx, es) || misaligned(dW, es) || misaligned(dbias, es) ||
+      misaligned(x_codes, 16) || misaligned(z_codes, 16) || misaligned(x_scales, 2) || misaligned(z_scales, 2))
+    return BCJR_ERR_INVALID_ARG;
+  if (M > 0 && (!dy || (dx && !W) || (dW && (!x_codes || !x_scales)) ||
+                (activation != kActNone && (!z_codes || !z_scales))))
+    return BCJR_ERR_INVALID_ARG;
+  const VjpPlan p = vjp_plan(dtype, M, N, activation);
+  if (p.total && (!workspace || misaligned(workspace, 16) || ws_bytes < p.total)) return BCJR_ERR_WORKSPACE;
+  return by_type(dtype, [&](auto t) -> int {
+    using T = decltype(t);
+    char* ws = static_cast<char*>(workspace);
+    const T* dz = static_cast<const T*>(dy);
+    int64_t ldz = ldd;
+    float* part = reinterpret_cast<float*>(ws + p.dz);
+    if (M > 0 && (activation != kActNone || dbias)) {
+      hipLaunchKernelGGL(dz_kernel<T>, group_grid(M, N, 64), dim3(64), 0, stream, static_cast<const T*>(dy), ldd,
+                         z_codes, z_scales, activation, M, N, reinterpret_cast<T*>(ws), dbias ? part : nullptr);
+      if (launched() != BCJR_OK) return BCJR_ERR_HIP;
+      if (activation != kActNone) {
+        dz = reinterpret_cast<const T*>(ws);
+        ldz = N;
+      }
+    }
+    if (dbias) {
+      hipLaunchKernelGGL(dbias_kernel<T>, dim3((unsigned)ceil_div(N, 64)), dim3(64), 0, stream, (const float*)part,
+                         ceil_div(M, kRows), N, static_cast<T*>(dbias));
+      if (launched() != BCJR_OK) return BCJR_ERR_HIP;
+    }
+    if (dx && M > 0) {
+      const GemmArgs g = {dz, W, ldz, ldw, nullptr, M, K, N, nullptr, nullptr, 0, dx, K, nullptr, nullptr, kActNone};
+      const int st = gemm<T, kRow, kCol>(g, stream);
+      if (st != BCJR_OK) return st;
+    }
+    if (dW) {
+      const GemmArgs g = {dz, x_codes, ldz, 0, x_scales, N, K, M, nullptr, nullptr, 0, dW, K, nullptr, nullptr, kActNone};
+      const int st = gemm<T, kCol, kCodes>(g, stream);
+      if (st != BCJR_OK) return st;
+    }
+    return BCJR_OK;
+  });
+}
+
+int64_t trellis_words(int state_bits, int k, int V, int64_t block) {
+  Code c;
+  return code_of(state_bits, k, V, block, &c) ? c.words : 0;
+}
+
+int trellis_pack(const int32_t* states, int64_t B, int64_t steps, int state_bits, int k, uint32_t* packed,
+                 int32_t* illegal, hipStream_t stream) {
+  Code c;
+  if (B < 0 || !code_of(state_bits, k, 1, steps, &c)) return BCJR_ERR_INVALID_ARG;
+  if (!threads_fit(B * c.words) || !threads_fit(B * steps)) return BCJR_ERR_UNSUPPORTED;
+  if ((B && (!states || !packed)) || misaligned(states, 4) || misaligned(packed, 4) || misaligned(illegal, 4))
+    return BCJR_ERR_INVALID_ARG;
+  if (illegal) {
+    hipLaunchKernelGGL(zero_kernel, dim3(1), dim3(1), 0, stream, illegal);
+    if (launched() != BCJR_OK) return BCJR_ERR_HIP;
+  }
+  if (B == 0) return BCJR_OK;
+  if (illegal) {
+    hipLaunchKernelGGL(pack_check_kernel, dim3((unsigned)ceil_div(B * steps, 256)), dim3(256), 0, stream, states, B,
+                       steps, c.n, c.k, illegal);
+    if (launched() != BCJR_OK) return BCJR_ERR_HIP;
+  }
+  hipLaunchKernelGGL(pack_kernel, dim3((unsigned)ceil_div(B * c.words, 256)), dim3(256), 0, stream, states, B, steps,
+                     c.n, c.k, c.words, packed);
+  return launched();
+}
+
+int trellis_unpack(const uint32_t* packed, int64_t B, int64_t steps, int state_bits, int k, int32_t* states,
+                   hipStream_t stream) {
+  Code c;
+  if (B < 0 || !code_of(state_bits, k, 1, steps, &c)) return BCJR_ERR_INVALID_ARG;
+  if (!threads_fit(B * steps)) return BCJR_ERR_UNSUPPORTED;
+  if ((B && (!states || !packed)) || misaligned(states, 4) || misaligned(packed, 4)) return BCJR_ERR_INVALID_ARG;
+  if (B == 0) return BCJR_OK;
+  hipLaunchKernelGGL(unpack_kernel, dim3((unsigned)ceil_div(B * steps, 256)), dim3(256), 0, stream, packed, B, steps,
+                     c.n, c.k, c.words, states);
+  return launched();
+}
+
+int trellis_dense(const uint32_t* packed, int64_t B, const float* codebook, int state_bits, int k, int V,
+                  int64_t block, const float* scales, void* W, int dtype, hipStream_t stream) {
+  Code c;
+  if (!dtype_ok(dtype) || B < 0 || !code_of(state_bits, k, V, block, &c)) return BCJR_ERR_INVALID_ARG;
+  if (!threads_fit(B * c.steps)) return BCJR_ERR_UNSUPPORTED;
+  if (!codebook || (B && (!W || !packed)) || misaligned(packed, 4) || misaligned(codebook, 16) ||
+      misaligned(scales, 4) || misaligned(W, elem_size(dtype)))
+    return BCJR_ERR_INVALID_ARG;
+  if (B == 0) return BCJR_OK;
+  return by_type(dtype, [&](auto t) -> int {
+    return run_dense(packed, codebook, scales, c, B, static_cast<decltype(t)*>(W), stream);
+  });
+}
+
+size_t trellis_linear_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K, int state_bits, int k, int V,
+                                      int64_t block) {
+  Code c;
+  if (!dtype_ok(dtype) || !dims_ok(M, N, K) || !dims_fit(M, N, K) || !code_of(state_bits, k, V, block, &c) ||
+      K % block)
+    return 0;
+  return align_up((size_t)(N * K) * elem_size(dtype));
+}
+
+int trellis_linear(const void* x, int64_t ldx, const uint32_t* packed, const float* codebook, int state_bits, int k,
+                   int V, int64_t block, const float* scales, const void* bias, const void* residual, int64_t ldr,
+                   int dtype, int activation, int64_t M, int64_t N, int64_t K, void* y, int64_t ldy,
+                   void* workspace, size_t ws_bytes, hipStream_t stream) {
+  Code c;
+  if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || !code_of(state_bits, k, V, block, &c) ||
+      K % block || ldx < K || ldy < N || (residual && ldr < N))
+    return BCJR_ERR_INVALID_ARG;
+  if (!dims_fit(M, N, K) || !threads_fit(N * K)) return BCJR_ERR_UNSUPPORTED;
+  if (M == 0) return BCJR_OK;
+  const size_t es = elem_size(dtype);
+  if (!x || !packed || !codebook || !y || misaligned(x, es) || misaligned(packed, 4) || misaligned(codebook, 16) ||
+      misaligned(scales, 4) || misaligned(bias, es) || misaligned(residual, es) || misaligned(y, es))
+    return BCJR_ERR_INVALID_ARG;
+  if (!workspace || misaligned(workspace, 16) ||
+      ws_bytes < trellis_linear_workspace_bytes(dtype, M, N, K, state_bits, k, V, block))
+    return BCJR_ERR_WORKSPACE;
+  return by_type(dtype, [&](auto t) -> int {
+    using T = decltype(t);
+    T* W = static_cast<T*>(workspace);
+    const int st = run_dense(packed, codebook, scales, c, N * (K / block), W, stream);
+    if (st != BCJR_OK) return st;
+    const GemmArgs g = {x, W, ldx, K, nullptr, M, N, K, bias, residual, ldr, y, ldy, nullptr, nullptr, activation};
+    return gemm<T, kRow, kRow>(g, stream);
+  });
+}
+
+}  // extern "C"

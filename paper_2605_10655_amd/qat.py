@@ -18,9 +18,13 @@ Options beyond the paper's runs, each named there:
 
 The loss is ||W_hat - W_target||_F^2, or with a proxy Hessian H = X^T X / n
 of layer inputs X the layer-output error tr((W_hat - W_t) H (W_hat - W_t)^T).
-Every trellis computation and every optimiser update runs in the library's
-HIP kernels; the loss residual and the product with H are plain tensor
-operations on the device.
+With the inputs X [n, cols] themselves it is the output error of the whole
+layer, ||f(X W_hat^T + b) - f(X W_t^T + b)||^2 / n, activation included: X is
+kept in 8 bits for the gradient (linear.Act8), and the final codeword is
+evaluated from its packed codes.
+Every trellis computation, every product of the layer and every optimiser
+update runs in the library's HIP kernels; the loss residual and the product
+with H are plain tensor operations on the device.
 """
 from __future__ import annotations
 
@@ -32,6 +36,7 @@ import torch
 from . import (bcjr_soft_codeword, bcjr_soft_codeword_vjp, bcjr_ste_vjp, bcjr_vec_soft_codeword,
                bcjr_vec_soft_codeword_vjp, bcjr_vec_viterbi_decode, qat_adam_step, qat_sgd_step,
                viterbi_decode)
+from .linear import act8_store, linear_act, linear_act_vjp, trellis_linear, trellis_pack
 
 __all__ = ["QATConfig", "QATResult", "anneal_temperatures", "drift_budget", "anneal_qat"]
 
@@ -86,6 +91,8 @@ class QATResult:
     loss_ptq: float              # loss of the Viterbi codeword of the initial W
     max_drift: float             # max |W - W_init| reached
     budget: dict                 # drift_budget() of the run's settings
+    packed: torch.Tensor = None  # W_hard's paths [rows, cols / block, words] (linear.trellis_linear);
+                                 # None where a block crosses rows
 
 
 def _loss_and_grad(W_hat, target, H):
@@ -96,16 +103,71 @@ def _loss_and_grad(W_hat, target, H):
     return float((RH * R).sum()), 2.0 * RH
 
 
-def anneal_qat(W_init, codebook, cfg: QATConfig, target=None, H=None, stream=None) -> QATResult:
+class _LayerLoss:
+    """||f(X W_hat^T + b) - f(X W_t^T + b)||^2 / n and its gradient in W_hat."""
+
+    def __init__(self, X, target, bias, activation, stream):
+        self.X, self.bias, self.act, self.stream = X, bias, activation, stream
+        self.x8 = act8_store(X, stream=stream)
+        self.Y = linear_act(X, target.to(X.dtype), bias, None, activation, stream=stream).float()
+
+    def of_output(self, Y) -> float:
+        R = Y.float() - self.Y
+        return float((R * R).sum()) / self.X.shape[0]
+
+    def of(self, W) -> float:
+        return self.of_output(linear_act(self.X, W.to(self.X.dtype), self.bias, None, self.act,
+                                         stream=self.stream))
+
+    def with_grad(self, W):
+        z8 = None
+        Wt = W.to(self.X.dtype)
+        Y = linear_act(self.X, Wt, self.bias, None, self.act, save=self.act != "none", stream=self.stream)
+        if self.act != "none":
+            Y, z8 = Y
+        R = Y.float() - self.Y
+        # half of the 1 / n goes to each side, so that neither the gradient
+        # nor the products leave a 16-bit type's range
+        half = 1.0 / math.sqrt(self.X.shape[0])
+        dW = linear_act_vjp((R * half).to(self.X.dtype), self.x8, Wt, z8, self.act, want_dx=False,
+                            want_dbias=False, stream=self.stream)[1]
+        return float((R * R).sum()) / self.X.shape[0], dW.float() * (2.0 * half)
+
+
+def anneal_qat(W_init, codebook, cfg: QATConfig, target=None, H=None, stream=None, X=None, bias=None,
+               activation="none") -> QATResult:
     """Run cfg.steps annealed steps on a [rows, cols] float32 device tensor.
 
     W_init is the starting pre-image (e.g. the weights themselves or a PTQ
     solution); target (default W_init) is what the codeword should
     reconstruct; H is an optional [cols, cols] proxy Hessian.  codebook is
     [S] (V = 1) or [S, V]; it is copied, and learned when
-    cfg.learn_codebook.
+    cfg.learn_codebook.  In place of H, X [tokens, cols] (float32, bfloat16
+    or float16) gives the loss on the layer's outputs, through bias [rows]
+    (X's type) and activation; the products then run in X's type.
     """
+    if stream is not None and stream != torch.cuda.current_stream(stream.device):
+        # the loss's tensor operations go to the current stream: make it the
+        # one asked for, and order it with the caller's on both sides
+        here = torch.cuda.current_stream(stream.device)
+        stream.wait_stream(here)
+        with torch.cuda.stream(stream):
+            res = anneal_qat(W_init, codebook, cfg, target, H, None, X, bias, activation)
+        here.wait_stream(stream)
+        for t in (res.W, res.codebook, res.W_hard, res.packed):
+            if t is not None:
+                t.record_stream(here)
+        return res
     n, k, V, blk = cfg.state_bits, cfg.k, cfg.V, cfg.block
+    if X is None and (bias is not None or activation != "none"):
+        raise ValueError("bias and activation belong to a loss on X")
+    if X is not None:
+        if H is not None:
+            raise ValueError("give H or X, not both")
+        if X.dim() != 2 or X.shape[0] < 1 or X.shape[1] != W_init.shape[-1]:
+            raise ValueError(f"X must be [tokens, {W_init.shape[-1]}], got {tuple(X.shape)}")
+        if W_init.shape[-1] % blk:
+            raise ValueError("a loss on X needs rows that are whole blocks")
     if W_init.dim() != 2 or W_init.numel() % blk:
         raise ValueError("W_init must be [rows, cols] with rows * cols a multiple of block")
     if cfg.optimizer not in ("adam", "sgd"):
@@ -117,6 +179,7 @@ def anneal_qat(W_init, codebook, cfg: QATConfig, target=None, H=None, stream=Non
     mc, vc = torch.zeros_like(c), torch.zeros_like(c)
     temps = anneal_temperatures(cfg.T0, cfg.T_end, cfg.steps)
     b1, b2 = cfg.betas
+    layer = None if X is None else _LayerLoss(X, target, bias, activation, stream)
 
     def forward(Wb, T):
         if cfg.ste:
@@ -140,7 +203,10 @@ def anneal_qat(W_init, codebook, cfg: QATConfig, target=None, H=None, stream=Non
     for i, T in enumerate(temps):
         Wb = W.view(-1, blk)
         fwd = forward(Wb, T)
-        loss, G = _loss_and_grad(fwd.view_as(W), target, H)
+        if layer is None:
+            loss, G = _loss_and_grad(fwd.view_as(W), target, H)
+        else:
+            loss, G = layer.with_grad(fwd.view_as(W))
         losses.append(loss)
         dW, dc = backward(Wb, T, G.contiguous().view(-1, blk), fwd)
         if cfg.optimizer == "adam":
@@ -157,15 +223,28 @@ def anneal_qat(W_init, codebook, cfg: QATConfig, target=None, H=None, stream=Non
     def snap(Wm, cb):
         Wb = Wm.contiguous().view(-1, blk)
         if V == 1:
-            return viterbi_decode(Wb, cb, n, k, stream=stream)[1].view_as(Wm)
-        return bcjr_vec_viterbi_decode(Wb, cb, n, k, V, stream=stream)[1].view_as(Wm)
+            states, hard = viterbi_decode(Wb, cb, n, k, stream=stream)
+        else:
+            states, hard = bcjr_vec_viterbi_decode(Wb, cb, n, k, V, stream=stream)
+        return states, hard.view_as(Wm)
 
-    W_hard = snap(W, c)
-    loss_hard = _loss_and_grad(W_hard, target, H)[0]
+    states, W_hard = snap(W, c)
+    packed = None
+    if W.shape[1] % blk == 0:
+        packed = trellis_pack(states.view(W.shape[0], W.shape[1] // blk, blk // V), n, k, check=False,
+                              stream=stream)
     # the PTQ reference: the initial weights snapped with the initial codebook
-    loss_ptq = _loss_and_grad(snap(W_init.detach(), codebook.detach().contiguous()), target, H)[0]
+    W_ptq = snap(W_init.detach(), codebook.detach().contiguous())[1]
+    if layer is None:
+        loss_hard = _loss_and_grad(W_hard, target, H)[0]
+        loss_ptq = _loss_and_grad(W_ptq, target, H)[0]
+    else:
+        loss_hard = layer.of_output(trellis_linear(X, packed, c, n, k, V, blk, bias=bias,
+                                                   activation=activation, stream=stream))
+        loss_ptq = layer.of(W_ptq)
     sigma = float(target.float().std())
     return QATResult(W=W, codebook=c, W_hard=W_hard, temps=temps, losses=losses,
                      loss_hard=loss_hard, loss_ptq=loss_ptq,
                      max_drift=float((W - W_init).abs().max()),
-                     budget=drift_budget(sigma, 1 << n, cfg.lr, cfg.steps, cfg.grad_clip))
+                     budget=drift_budget(sigma, 1 << n, cfg.lr, cfg.steps, cfg.grad_clip),
+                     packed=packed)
