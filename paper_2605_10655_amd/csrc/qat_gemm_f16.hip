@@ -1,0 +1,15 @@
+// qat_gemm_f16.hip -- the products of qat_gemm_launch.h in f16: forward (row,
+// row), gradient of x (row, col), gradient of W (col, codes).
+#include <hip/hip_runtime.h>
+
+#include "qat_gemm_launch.h"
+
+namespace bcjr {
+namespace qlin {
+
+template int gemm<f16, kRow, kRow>(GemmArgs, void*, hipStream_t);
+template int gemm<f16, kRow, kCol>(GemmArgs, void*, hipStream_t);
+template int gemm<f16, kCol, kCodes>(GemmArgs, void*, hipStream_t);
+
+}  // namespace qlin
+}  // namespace bcjr

@@ -1,0 +1,15 @@
+// qat_gemm_f32.hip -- the products of qat_gemm_launch.h in float: forward (row,
+// row), gradient of x (row, col), gradient of W (col, codes).
+#include <hip/hip_runtime.h>
+
+#include "qat_gemm_launch.h"
+
+namespace bcjr {
+namespace qlin {
+
+template int gemm<float, kRow, kRow>(GemmArgs, void*, hipStream_t);
+template int gemm<float, kRow, kCol>(GemmArgs, void*, hipStream_t);
+template int gemm<float, kCol, kCodes>(GemmArgs, void*, hipStream_t);
+
+}  // namespace qlin
+}  // namespace bcjr

@@ -1,0 +1,102 @@
+// qat_gemm_launch.h -- choice of the product's tile and split, and its launch.
+// Instantiated for one type in each of qat_gemm_{bf16,f16,f32}.hip.
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+#include "bcjr.h"
+#include "qat_gemm_kernels.h"
+
+namespace bcjr {
+namespace qlin {
+
+constexpr size_t kAlign = 256;
+inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+inline bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+inline int launched() { return hipGetLastError() == hipSuccess ? BCJR_OK : BCJR_ERR_HIP; }
+
+
+inline dim3 group_grid(int64_t rows, int64_t cols, int threads) {
+  return dim3((unsigned)ceil_div(rows, kRows), (unsigned)ceil_div(cols, threads));
+}
+
+// A product's tile and its split of k.
+struct GemmPlan {
+  int tile;        // 256, 128 or 64
+  int ti, tj;      // tiles
+  int splits;
+  size_t part;     // bytes of the partial sums
+};
+
+inline GemmPlan gemm_plan(int dtype, int64_t I, int64_t J, int64_t K) {
+  GemmPlan p;
+  p.tile = 64;
+  for (int t : {256, 128})
+    if (ceil_div(I, t) * ceil_div(J, t) >= 200) {
+      p.tile = t;
+      break;
+    }
+  p.ti = (int)ceil_div(I, p.tile);
+  p.tj = (int)ceil_div(J, p.tile);
+  const int64_t steps = ceil_div(K, dtype == kF32 ? 32 : 64), tiles = (int64_t)p.ti * p.tj;
+  p.splits = 1;
+  if (tiles < 200) {
+    const int64_t by_fill = 256 / tiles, by_length = steps / 8;
+    p.splits = (int)(by_fill < by_length ? by_fill : by_length);
+    if (p.splits < 1) p.splits = 1;
+  }
+  p.part = p.splits > 1 ? align_up((size_t)p.splits * I * J * sizeof(float)) : 0;
+  return p;
+}
+
+template <class T, int AM, int BM, int BT, int WI, int WJ, bool COPY>
+void launch_gemm(const GemmArgs& g, const GemmPlan& p, hipStream_t stream) {
+  hipLaunchKernelGGL((gemm_kernel<T, AM, BM, BT, BT, WI, WJ, COPY>), dim3((unsigned)(p.ti * p.tj * p.splits)),
+                     dim3(BT / WI * (BT / WJ) * 64), 0, stream, g, p.ti, p.tj);
+}
+
+// whether tiles of an operand can be copied straight into LDS (Tile::copy)
+inline bool copies(int mode, const void* p, int64_t ld, int64_t rows, int64_t K, int es, int tile) {
+  if (mode == kCodes) return true;
+  const int e = 16 / es;
+  return !misaligned(p, 16) && ld % e == 0 && (mode == kRow ? K : rows) % e == 0 &&
+         (int64_t)(mode == kRow ? tile : 8 * e) * ld * es < ((int64_t)1 << 31);
+}
+
+// The product and its epilogue (of zero sums where K == 0).
+template <class T, int AM, int BM>
+int gemm(GemmArgs g, void* ws, hipStream_t stream) {
+  if (g.I == 0 || g.J == 0) return BCJR_OK;
+  constexpr int es = (int)sizeof(T), dtype = es == 4 ? kF32 : kBF16;
+  GemmPlan p = gemm_plan(dtype, g.I, g.J, g.K);
+  if ((int64_t)p.ti * p.tj * 4 * p.splits >= ((int64_t)1 << 31)) return BCJR_ERR_UNSUPPORTED;   // one grid
+  g.splits = p.splits;
+  g.part = static_cast<float*>(ws);
+  if (copies(AM, g.a, g.lda, g.I, g.K, es, p.tile) && copies(BM, g.b, g.ldb, g.J, g.K, es, p.tile)) {
+    if (p.tile == 256) launch_gemm<T, AM, BM, 256, 128, 64, true>(g, p, stream);
+    else if (p.tile == 128) launch_gemm<T, AM, BM, 128, 64, 64, true>(g, p, stream);
+    else launch_gemm<T, AM, BM, 64, 32, 32, true>(g, p, stream);
+  } else {
+    if (p.tile == 256) {   // both tiles through registers do not fit them (k is not split here)
+      p.ti = (int)ceil_div(g.I, 128);
+      p.tj = (int)ceil_div(g.J, 128);
+    }
+    if (p.tile >= 128) launch_gemm<T, AM, BM, 128, 64, 64, false>(g, p, stream);
+    else launch_gemm<T, AM, BM, 64, 32, 32, false>(g, p, stream);
+  }
+  if (launched() != BCJR_OK) return BCJR_ERR_HIP;
+  if (p.splits > 1) {
+    if (g.zcodes)
+      hipLaunchKernelGGL((join_kernel<T, true>), group_grid(g.I, g.J, 64), dim3(64), 0, stream, g);
+    else
+      hipLaunchKernelGGL((join_kernel<T, false>), dim3((unsigned)g.I, (unsigned)ceil_div(g.J, 256)), dim3(256), 0,
+                         stream, g);
+    return launched();
+  }
+  return BCJR_OK;
+}
+
+}  // namespace qlin
+}  // namespace bcjr

@@ -7,15 +7,22 @@
 #include <cstdint>
 
 #include "bcjr.h"
+#include "qat_gemm_launch.h"
 #include "qat_linear_kernels.h"
 
 namespace bcjr {
 namespace qlin {
-namespace {
 
-constexpr size_t kAlign = 256;
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+#define QAT_GEMM_EXTERN(T)                                                   \
+  extern template int gemm<T, kRow, kRow>(GemmArgs, void*, hipStream_t);     \
+  extern template int gemm<T, kRow, kCol>(GemmArgs, void*, hipStream_t);     \
+  extern template int gemm<T, kCol, kCodes>(GemmArgs, void*, hipStream_t);
+QAT_GEMM_EXTERN(bf16)
+QAT_GEMM_EXTERN(f16)
+QAT_GEMM_EXTERN(float)
+#undef QAT_GEMM_EXTERN
+
+namespace {
 
 // Limits of the grids: columns of any operand lie along a grid's second axis.
 constexpr int64_t kMaxRows = (int64_t)1 << 31, kMaxCols = (int64_t)1 << 22;
@@ -23,11 +30,8 @@ constexpr int64_t kMaxRows = (int64_t)1 << 31, kMaxCols = (int64_t)1 << 22;
 int elem_size(int dtype) { return dtype == kF32 ? 4 : 2; }
 bool dtype_ok(int dtype) { return dtype == kF32 || dtype == kBF16 || dtype == kF16; }
 bool act_ok(int act) { return act >= kActNone && act <= kActGeluTanh; }
-bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 bool dims_ok(int64_t M, int64_t N, int64_t K) { return M >= 0 && N >= 1 && K >= 1; }
 bool dims_fit(int64_t M, int64_t N, int64_t K) { return M < kMaxRows && N < kMaxCols && K < kMaxCols; }
-int launched() { return hipGetLastError() == hipSuccess ? BCJR_OK : BCJR_ERR_HIP; }
-
 template <class F>
 int by_type(int dtype, F f) {
   if (dtype == kBF16) return f(bf16());
@@ -35,31 +39,22 @@ int by_type(int dtype, F f) {
   return f(float());
 }
 
-dim3 group_grid(int64_t rows, int64_t cols, int threads) {
-  return dim3((unsigned)ceil_div(rows, kRows), (unsigned)ceil_div(cols, threads));
-}
-
-template <class T, int AM, int BM>
-int gemm(const GemmArgs& g, hipStream_t stream) {
-  if (g.I == 0 || g.J == 0) return BCJR_OK;
-  hipLaunchKernelGGL((gemm_kernel<T, AM, BM>), dim3((unsigned)ceil_div(g.I, kTile), (unsigned)ceil_div(g.J, kTile)),
-                     dim3(256), 0, stream, g);
-  return launched();
-}
-
-int run_linear(const GemmArgs& g, int dtype, hipStream_t stream) {
-  return by_type(dtype, [&](auto t) -> int { return gemm<decltype(t), kRow, kRow>(g, stream); });
+int run_linear(const GemmArgs& g, int dtype, void* ws, hipStream_t stream) {
+  return by_type(dtype, [&](auto t) -> int { return gemm<decltype(t), kRow, kRow>(g, ws, stream); });
 }
 
 struct VjpPlan {
-  size_t dz, part, total;
+  size_t dz, part, sums, total;
 };
 
-VjpPlan vjp_plan(int dtype, int64_t M, int64_t N, int act) {
+// dz, the groups' sums of dbias, then the partial sums of the products
+VjpPlan vjp_plan(int dtype, int64_t M, int64_t N, int64_t K, int act) {
   VjpPlan p;
   p.dz = act == kActNone ? 0 : align_up((size_t)(M * N) * elem_size(dtype));
   p.part = align_up((size_t)(ceil_div(M, kRows) * N) * sizeof(float));
-  p.total = p.dz + p.part;
+  const size_t dx = M ? gemm_plan(dtype, M, K, N).part : 0, dW = gemm_plan(dtype, N, K, M).part;
+  p.sums = dx > dW ? dx : dW;
+  p.total = p.dz + p.part + p.sums;
   return p;
 }
 
@@ -132,8 +127,8 @@ int qat_act8_load(const int8_t* codes, const uint16_t* scales, int64_t rows, int
 }
 
 size_t qat_linear_act_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K) {
-  (void)dtype, (void)M, (void)N, (void)K;
-  return 0;
+  if (!dtype_ok(dtype) || !dims_ok(M, N, K) || !dims_fit(M, N, K) || M == 0) return 0;
+  return gemm_plan(dtype, M, N, K).part;
 }
 
 int qat_linear_act(const void* x, int64_t ldx, const void* W, int64_t ldw, const void* bias, const void* residual,
@@ -151,12 +146,12 @@ int qat_linear_act(const void* x, int64_t ldx, const void* W, int64_t ldw, const
   const size_t need = qat_linear_act_workspace_bytes(dtype, M, N, K);
   if (need && (!workspace || misaligned(workspace, 16) || ws_bytes < need)) return BCJR_ERR_WORKSPACE;
   const GemmArgs g = {x, W, ldx, ldw, nullptr, M, N, K, bias, residual, ldr, y, ldy, z_codes, z_scales, activation};
-  return run_linear(g, dtype, stream);
+  return run_linear(g, dtype, workspace, stream);
 }
 
 size_t qat_linear_act_vjp_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K, int activation) {
   if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || !dims_fit(M, N, K)) return 0;
-  return vjp_plan(dtype, M, N, activation).total;
+  return vjp_plan(dtype, M, N, K, activation).total;
 }
 
 int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const uint16_t* x_scales, const void* W,
@@ -174,7 +169,7 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
   if (M > 0 && (!dy || (dx && !W) || (dW && (!x_codes || !x_scales)) ||
                 (activation != kActNone && (!z_codes || !z_scales))))
     return BCJR_ERR_INVALID_ARG;
-  const VjpPlan p = vjp_plan(dtype, M, N, activation);
+  const VjpPlan p = vjp_plan(dtype, M, N, K, activation);
   if (p.total && (!workspace || misaligned(workspace, 16) || ws_bytes < p.total)) return BCJR_ERR_WORKSPACE;
   return by_type(dtype, [&](auto t) -> int {
     using T = decltype(t);
@@ -198,12 +193,12 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
     }
     if (dx && M > 0) {
       const GemmArgs g = {dz, W, ldz, ldw, nullptr, M, K, N, nullptr, nullptr, 0, dx, K, nullptr, nullptr, kActNone};
-      const int st = gemm<T, kRow, kCol>(g, stream);
+      const int st = gemm<T, kRow, kCol>(g, ws + p.dz + p.part, stream);
       if (st != BCJR_OK) return st;
     }
     if (dW) {
       const GemmArgs g = {dz, x_codes, ldz, 0, x_scales, N, K, M, nullptr, nullptr, 0, dW, K, nullptr, nullptr, kActNone};
-      const int st = gemm<T, kCol, kCodes>(g, stream);
+      const int st = gemm<T, kCol, kCodes>(g, ws + p.dz + p.part, stream);
       if (st != BCJR_OK) return st;
     }
     return BCJR_OK;
@@ -269,7 +264,7 @@ size_t trellis_linear_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K
   if (!dtype_ok(dtype) || !dims_ok(M, N, K) || !dims_fit(M, N, K) || !code_of(state_bits, k, V, block, &c) ||
       K % block)
     return 0;
-  return align_up((size_t)(N * K) * elem_size(dtype));
+  return align_up((size_t)(N * K) * elem_size(dtype)) + (M ? gemm_plan(dtype, M, N, K).part : 0);
 }
 
 int trellis_linear(const void* x, int64_t ldx, const uint32_t* packed, const float* codebook, int state_bits, int k,
@@ -295,7 +290,7 @@ int trellis_linear(const void* x, int64_t ldx, const uint32_t* packed, const flo
     const int st = run_dense(packed, codebook, scales, c, N * (K / block), W, stream);
     if (st != BCJR_OK) return st;
     const GemmArgs g = {x, W, ldx, K, nullptr, M, N, K, bias, residual, ldr, y, ldy, nullptr, nullptr, activation};
-    return gemm<T, kRow, kRow>(g, stream);
+    return gemm<T, kRow, kRow>(g, reinterpret_cast<char*>(W) + align_up((size_t)(N * K) * es), stream);
   });
 }
 

@@ -138,6 +138,18 @@ def test_linear_sizes(t, M, N, K):
     _check_linear(host, devi, "silu", R.TYPES[t], f"{t} {M}x{N}x{K}")
 
 
+# the tiles of large products, whole ones and ragged ones, aligned and not
+LARGE = [(1930, 2056, 136, 8), (1930, 2051, 75, 3), (3900, 3592, 72, 0), (3841, 3587, 70, 1)]
+
+
+@pytest.mark.parametrize("t", R.TYPES)
+@pytest.mark.parametrize("M,N,K,pad", LARGE)
+def test_linear_large_tiles(t, M, N, K, pad):
+    _say(f"[linear large] {t} {M}x{N}x{K} pad {pad}")
+    host, devi = _layer(M + N, M, N, K, R.TYPES[t], pad)
+    _check_linear(host, devi, "gelu_tanh", R.TYPES[t], f"{t} {M}x{N}x{K}")
+
+
 @pytest.mark.parametrize("t", R.TYPES)
 @pytest.mark.parametrize("act", R.ACTS)
 @pytest.mark.parametrize("M,pad,bias,residual", [(1, 0, True, False), (5, 8, False, True), (70, 3, True, True),
@@ -189,14 +201,19 @@ def test_linear_repeats_bit_for_bit():
 
 
 # ---------------------------------------------------------------- backward
-def _vjp_case(seed, M, N, K, dt, act, pad=0):
+def _vjp_case(seed, M, N, K, dt, act, pad=0, dense=False):
+    """Reference and arguments; dense: the checkpoints' values as the GPU
+    reads them back (test_act8_equals_the_definition holds them to the
+    definition), which is quick for large ones."""
     x, xd = rand(seed, M, K, dtype=dt)
     W, Wd = rand(seed + 1, N, K, dtype=dt, scale=N ** -0.5, pad=pad)
     dy, dyd = rand(seed + 2, M, N, dtype=dt, scale=M ** -0.5, pad=pad)
     z, zd = rand(seed + 3, M, N, scale=2.0)
     x8, z8 = Q.act8_store(xd), Q.act8_store(zd) if act != "none" else None
-    xv = R.act8_64(x, dt == torch.float16)[2]
-    zv = R.act8_64(z)[2]
+    if dense:
+        xv, zv = Q.act8_load(x8).cpu(), Q.act8_load(z8).cpu()
+    else:
+        xv, zv = R.act8_64(x, dt == torch.float16)[2], R.act8_64(z)[2]
     return R.vjp64(dy, xv, W, zv, act, dt), (dyd, x8, Wd, z8, act)
 
 
@@ -207,6 +224,17 @@ def test_vjp_sizes(t, M, N, K):
     ref, call = _vjp_case(M + 3 * N, M, N, K, R.TYPES[t], "silu")
     for got, r, b, what in zip(Q.linear_act_vjp(*call), ref[::2], ref[1::2], ("dx", "dW", "dbias")):
         within(got, r, b, f"{what} {t} {M}x{N}x{K}")
+
+
+@pytest.mark.parametrize("t", R.TYPES)
+@pytest.mark.parametrize("I,J,K,pad", LARGE)
+def test_vjp_large_tiles(t, I, J, K, pad):
+    """dx with few outputs to sum over, dW with few tokens."""
+    for M, N, C in ((I, K, J), (K, I, J)):
+        _say(f"[vjp large] {t} {M}x{N}x{C} pad {pad}")
+        ref, call = _vjp_case(M + N, M, N, C, R.TYPES[t], "gelu", pad, dense=True)
+        for got, r, b, what in zip(Q.linear_act_vjp(*call), ref[::2], ref[1::2], ("dx", "dW", "dbias")):
+            within(got, r, b, f"{what} {t} {M}x{N}x{C}")
 
 
 @pytest.mark.parametrize("t", R.TYPES)
