@@ -95,9 +95,23 @@ __device__ __forceinline__ float logistic(float z) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
 }
 
+// The normal distribution's Phi(z), and e = exp(-z^2 / 2): Phi(-|z|) = erfc(|z|
+// / sqrt 2) / 2 by the polynomial of Abramowitz & Stegun 7.1.26 (erf within
+// 1.5e-7), without a branch.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * 0.70710678118654752f * fabsf(z));
+  e = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
+  const float q = 0.5f * e * t *
+                  (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+  return z < 0.f ? q : 1.f - q;
+}
+
 __device__ __forceinline__ float act_value(float z, int act) {
   if (act == kActSilu) return z * logistic(z);
-  if (act == kActGelu) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+  if (act == kActGelu) {
+    float e;
+    return z * normal_cdf(z, e);
+  }
   if (act == kActGeluTanh) {
     // 0.5 (1 + tanh u) = 1 / (1 + e^(-2u))
     const float u = 0.79788456080286536f * (z + 0.044715f * z * z * z);
@@ -114,8 +128,11 @@ __device__ __forceinline__ float act_slope(float z, int act) {
     const float p = logistic(z);
     return p * (1.f + z * (1.f - p));
   }
-  if (act == kActGelu)
-    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+  if (act == kActGelu) {
+    float e;
+    const float p = normal_cdf(z, e);
+    return p + z * e * 0.39894228040143268f;
+  }
   if (act == kActGeluTanh) {
     const float u = 0.79788456080286536f * (z + 0.044715f * z * z * z);
     const float s = logistic(2.f * u);

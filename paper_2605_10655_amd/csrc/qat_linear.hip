@@ -39,6 +39,16 @@ int by_type(int dtype, F f) {
   return f(float());
 }
 
+template <class T>
+dim3 band_grid(int64_t rows, int64_t cols) {
+  return dim3((unsigned)(ceil_div(rows, kRows) * ceil_div(cols, kGroupThreads * kCols<T>)));
+}
+
+// workgroups of 32 rows and at least 256 columns that one launch can have
+bool bands_fit(int64_t rows, int64_t cols) {
+  return ceil_div(rows, kRows) * ceil_div(cols, kGroupThreads) < ((int64_t)1 << 31);
+}
+
 int run_linear(const GemmArgs& g, int dtype, void* ws, hipStream_t stream) {
   return by_type(dtype, [&](auto t) -> int { return gemm<decltype(t), kRow, kRow>(g, ws, stream); });
 }
@@ -98,13 +108,13 @@ extern "C" {
 int qat_act8_store(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t* codes,
                    uint16_t* scales, hipStream_t stream) {
   if (!dtype_ok(dtype) || rows < 0 || cols < 1 || ldx < cols) return BCJR_ERR_INVALID_ARG;
-  if (rows >= kMaxRows || cols >= kMaxCols) return BCJR_ERR_UNSUPPORTED;
+  if (rows >= kMaxRows || cols >= kMaxCols || !bands_fit(rows, cols)) return BCJR_ERR_UNSUPPORTED;
   if (rows == 0) return BCJR_OK;
   if (!x || !codes || !scales || misaligned(x, elem_size(dtype)) || misaligned(codes, 16) || misaligned(scales, 2))
     return BCJR_ERR_INVALID_ARG;
   return by_type(dtype, [&](auto t) -> int {
     using T = decltype(t);
-    hipLaunchKernelGGL(act8_store_kernel<T>, group_grid(rows, cols, 64), dim3(64), 0, stream,
+    hipLaunchKernelGGL(act8_store_kernel<T>, band_grid<T>(rows, cols), dim3(kGroupThreads), 0, stream,
                        static_cast<const T*>(x), rows, cols, ldx, codes, scales);
     return launched();
   });
@@ -113,14 +123,14 @@ int qat_act8_store(const void* x, int dtype, int64_t rows, int64_t cols, int64_t
 int qat_act8_load(const int8_t* codes, const uint16_t* scales, int64_t rows, int64_t cols, void* out, int dtype,
                   int64_t ldo, hipStream_t stream) {
   if (!dtype_ok(dtype) || rows < 0 || cols < 1 || ldo < cols) return BCJR_ERR_INVALID_ARG;
-  if (rows >= kMaxRows || cols >= kMaxCols) return BCJR_ERR_UNSUPPORTED;
+  if (rows >= kMaxRows || cols >= kMaxCols || !bands_fit(rows, cols)) return BCJR_ERR_UNSUPPORTED;
   if (rows == 0) return BCJR_OK;
   if (!out || !codes || !scales || misaligned(out, elem_size(dtype)) || misaligned(codes, 16) ||
       misaligned(scales, 2))
     return BCJR_ERR_INVALID_ARG;
   return by_type(dtype, [&](auto t) -> int {
     using T = decltype(t);
-    hipLaunchKernelGGL(act8_load_kernel<T>, group_grid(rows, cols, 64), dim3(64), 0, stream, codes, scales, rows,
+    hipLaunchKernelGGL(act8_load_kernel<T>, band_grid<T>(rows, cols), dim3(kGroupThreads), 0, stream, codes, scales, rows,
                        cols, static_cast<T*>(out), ldo);
     return launched();
   });
@@ -160,7 +170,7 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
                        size_t ws_bytes, hipStream_t stream) {
   if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || ldd < N || (dx && ldw < K))
     return BCJR_ERR_INVALID_ARG;
-  if (!dims_fit(M, N, K)) return BCJR_ERR_UNSUPPORTED;
+  if (!dims_fit(M, N, K) || !bands_fit(M, N)) return BCJR_ERR_UNSUPPORTED;
   if (!dx && !dW && !dbias) return BCJR_OK;
   const size_t es = elem_size(dtype);
   if (misaligned(dy, es) || misaligned(W, es) || misaligned(dx, es) || misaligned(dW, es) || misaligned(dbias, es) ||
@@ -178,8 +188,12 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
     int64_t ldz = ldd;
     float* part = reinterpret_cast<float*>(ws + p.dz);
     if (M > 0 && (activation != kActNone || dbias)) {
-      hipLaunchKernelGGL(dz_kernel<T>, group_grid(M, N, 64), dim3(64), 0, stream, static_cast<const T*>(dy), ldd,
-                         z_codes, z_scales, activation, M, N, reinterpret_cast<T*>(ws), dbias ? part : nullptr);
+      const auto kernel = activation == kActNone   ? dz_kernel<T, kActNone>
+                          : activation == kActSilu ? dz_kernel<T, kActSilu>
+                          : activation == kActGelu ? dz_kernel<T, kActGelu>
+                                                   : dz_kernel<T, kActGeluTanh>;
+      hipLaunchKernelGGL(kernel, band_grid<T>(M, N), dim3(kGroupThreads), 0, stream, static_cast<const T*>(dy), ldd,
+                         z_codes, z_scales, M, N, reinterpret_cast<T*>(ws), dbias ? part : nullptr);
       if (launched() != BCJR_OK) return BCJR_ERR_HIP;
       if (activation != kActNone) {
         dz = reinterpret_cast<const T*>(ws);
@@ -187,7 +201,7 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
       }
     }
     if (dbias) {
-      hipLaunchKernelGGL(dbias_kernel<T>, dim3((unsigned)ceil_div(N, 64)), dim3(64), 0, stream, (const float*)part,
+      hipLaunchKernelGGL(dbias_kernel<T>, dim3((unsigned)ceil_div(N, 64)), dim3(1024), 0, stream, (const float*)part,
                          ceil_div(M, kRows), N, static_cast<T*>(dbias));
       if (launched() != BCJR_OK) return BCJR_ERR_HIP;
     }

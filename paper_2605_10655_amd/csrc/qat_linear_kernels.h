@@ -8,91 +8,215 @@ namespace bcjr {
 namespace qlin {
 
 // ---------------------------------------------------------------- 8-bit checkpoints
-// One thread per group: 32 rows of one column, read coalesced over the
-// columns, 32 codes written as 32 contiguous bytes.
+// Rows of two neighbouring 16-bit columns (one of 32 bits) per thread: a wave
+// then moves 256 contiguous bytes of each row, and both columns' codes are 64
+// contiguous bytes.  Workgroups of one band of 32 rows are neighbours, so that
+// whole rows of memory are open at a time.
 template <class T>
-__global__ void act8_store_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ldx,
-                                  int8_t* __restrict__ codes, uint16_t* __restrict__ scales) {
-  const int64_t c = (int64_t)blockIdx.y * blockDim.x + threadIdx.x;
-  const int64_t g = blockIdx.x;
-  if (c >= cols) return;
-  float v[kRows];
-  float amax = 0.f;
-  bool bad = false;
+constexpr int kCols = 4 / (int)sizeof(T);
+constexpr int kGroupThreads = 64;
+
+struct Band {
+  int64_t g, c;
+  int n;            // columns of this thread: none past the edge
+};
+
+template <int C>
+__device__ __forceinline__ Band band_of(int64_t cols) {
+  const uint32_t per = (uint32_t)((cols + kGroupThreads * C - 1) / (kGroupThreads * C));
+  const uint32_t id = blockIdx.x;
+  Band b;
+  b.g = id / per;
+  b.c = ((int64_t)(id % per) * kGroupThreads + threadIdx.x) * C;
+  b.n = b.c >= cols ? 0 : (cols - b.c < C ? (int)(cols - b.c) : C);
+  return b;
+}
+
+// n <= C values at p, which need not be aligned
+template <class T, int C>
+__device__ __forceinline__ void get(const T* p, int n, float* v) {
+  T t[C] = {};
+  if (n == C)
+    __builtin_memcpy(t, p, sizeof(t));
+  else
+    t[0] = p[0];
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int64_t r = g * kRows + i;
-    v[i] = r < rows ? (float)x[r * ldx + c] : 0.f;
-    if (finite_bits(v[i]))
-      amax = fmaxf(amax, fabsf(v[i]));
-    else
-      bad = true;
+  for (int c = 0; c < C; ++c) v[c] = (float)t[c];
+}
+
+template <class T, int C>
+__device__ __forceinline__ void set(T* p, int n, const float* v) {
+  T t[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) t[c] = (T)v[c];
+  if (n == C)
+    __builtin_memcpy(p, t, sizeof(t));
+  else
+    p[0] = t[0];
+}
+
+// N rows of a band, zeros past the last: all loads under way at once
+template <class T, int C, int N>
+__device__ __forceinline__ void get_rows(const T* p, int64_t ld, int left, int n, float (*v)[C]) {
+  if (left >= N && n == C) {
+    T t[N][C];
+#pragma unroll
+    for (int i = 0; i < N; ++i) __builtin_memcpy(t[i], p + i * ld, sizeof(t[i]));
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int c = 0; c < C; ++c) v[i][c] = (float)t[i][c];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) v[i][c] = 0.f;
+      if (i < left) get<T, C>(p + i * ld, n, v[i]);
+    }
   }
-  const Q8 q = q8_of(amax, kEmin<T>, kEmax<T>);
-  uint32_t w[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    w[i] = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[i] |= (uint32_t)(q8_code(v[4 * i + j], q) & 255) << (8 * j);
-  }
-  const int64_t at = g * cols + c;
-  u32x4* o = reinterpret_cast<u32x4*>(codes + at * kRows);
-  o[0] = u32x4{w[0], w[1], w[2], w[3]};
-  o[1] = u32x4{w[4], w[5], w[6], w[7]};
-  scales[at] = q8_scale_bits(q, bad);
+}
+
+__device__ __forceinline__ int code_at(const u32x4* w, int i) {
+  return (int)(w[i >> 4][(i >> 2) & 3] << (24 - 8 * (i & 3))) >> 24;
 }
 
 template <class T>
-__global__ void act8_load_kernel(const int8_t* __restrict__ codes, const uint16_t* __restrict__ scales,
-                                 int64_t rows, int64_t cols, T* __restrict__ out, int64_t ldo) {
-  const int64_t c = (int64_t)blockIdx.y * blockDim.x + threadIdx.x;
-  const int64_t g = blockIdx.x;
-  if (c >= cols) return;
-  const int64_t at = g * cols + c;
-  const uint16_t s = scales[at];
+__global__ __launch_bounds__(kGroupThreads) void act8_store_kernel(const T* __restrict__ x, int64_t rows,
+                                                                   int64_t cols, int64_t ldx,
+                                                                   int8_t* __restrict__ codes,
+                                                                   uint16_t* __restrict__ scales) {
+  constexpr int C = kCols<T>;
+  const Band b = band_of<C>(cols);
+  if (b.n == 0) return;
+  float v[kRows][C], amax[C] = {};
+  bool bad[C] = {};
+  const T* src = x + b.g * kRows * ldx + b.c;
+  const int left = rows - b.g * kRows < kRows ? (int)(rows - b.g * kRows) : kRows;
+  get_rows<T, C, kRows>(src, ldx, left, b.n, v);
+#pragma unroll
+  for (int i = 0; i < kRows; ++i)
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const bool fin = finite_bits(v[i][c]);
+      amax[c] = fmaxf(amax[c], fin ? fabsf(v[i][c]) : 0.f);
+      bad[c] |= !fin;
+    }
+  const int64_t at = b.g * cols + b.c;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    if (c >= b.n) break;
+    const Q8 q = q8_of(amax[c], kEmin<T>, kEmax<T>);
+    u32x4* o = reinterpret_cast<u32x4*>(codes + (at + c) * kRows);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4 w = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i >> 2] |= (uint32_t)(q8_code(v[16 * h + i][c], q) & 255) << (8 * (i & 3));
+      o[h] = w;
+    }
+    scales[at + c] = q8_scale_bits(q, bad[c]);
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(kGroupThreads) void act8_load_kernel(const int8_t* __restrict__ codes,
+                                                                  const uint16_t* __restrict__ scales, int64_t rows,
+                                                                  int64_t cols, T* __restrict__ out, int64_t ldo) {
+  constexpr int C = kCols<T>;
+  const Band b = band_of<C>(cols);
+  if (b.n == 0) return;
+  const int64_t at = b.g * cols + b.c;
+  u32x4 w[C][2];
+  uint16_t s[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int64_t o = at + (c < b.n ? c : 0);
+    s[c] = scales[o];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w[c][h] = reinterpret_cast<const u32x4*>(codes + o * kRows)[h];
+  }
+  T* dst = out + b.g * kRows * ldo + b.c;
+  const int left = rows - b.g * kRows < kRows ? (int)(rows - b.g * kRows) : kRows;
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
-    const int64_t r = g * kRows + i;
-    if (r < rows) out[r * ldo + c] = (T)q8_value(codes[at * kRows + i], s);
+    if (i < left) {
+      float v[C];
+#pragma unroll
+      for (int c = 0; c < C; ++c) v[c] = q8_value(code_at(w[c], i), s[c]);
+      set<T, C>(dst + i * ldo, b.n, v);
+    }
   }
 }
 
 // ---------------------------------------------------------------- backward
 // dz = dy * act'(z8), rounded to T for the matrix instructions (half a step of
 // the type each, as dy itself), and the sum of the unrounded dz over each
-// group's rows.  One thread per group.
-template <class T>
-__global__ void dz_kernel(const T* __restrict__ dy, int64_t ldd, const int8_t* __restrict__ zcodes,
-                          const uint16_t* __restrict__ zscales, int act, int64_t rows, int64_t cols,
-                          T* __restrict__ dz, float* __restrict__ part) {
-  const int64_t c = (int64_t)blockIdx.y * blockDim.x + threadIdx.x;
-  const int64_t g = blockIdx.x;
-  if (c >= cols) return;
-  const int64_t at = g * cols + c;
-  const uint16_t s = act != kActNone ? zscales[at] : (uint16_t)0;
-  float sum = 0.f;
+// group's rows.
+template <class T, int ACT>
+__global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__ dy, int64_t ldd,
+                                                           const int8_t* __restrict__ zcodes,
+                                                           const uint16_t* __restrict__ zscales, int64_t rows,
+                                                           int64_t cols, T* __restrict__ dz,
+                                                           float* __restrict__ part) {
+  constexpr int C = kCols<T>;
+  const Band b = band_of<C>(cols);
+  if (b.n == 0) return;
+  const int64_t at = b.g * cols + b.c;
+  const int left = rows - b.g * kRows < kRows ? (int)(rows - b.g * kRows) : kRows;
+  float sum[C] = {};
+  u32x4 w[C][2];
+  uint16_t s[C];
+  if (ACT != kActNone)
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int64_t r = g * kRows + i;
-    if (r >= rows) break;
-    float v = (float)dy[r * ldd + c];
-    if (act != kActNone) {
-      v *= act_slope(q8_value(zcodes[at * kRows + i], s), act);
-      dz[r * cols + c] = (T)v;
+    for (int c = 0; c < C; ++c) {
+      const int64_t o = at + (c < b.n ? c : 0);
+      s[c] = zscales[o];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) w[c][h] = reinterpret_cast<const u32x4*>(zcodes + o * kRows)[h];
     }
-    sum += v;
+  // 16 rows at a time: their loads together, then their products
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int64_t r0 = b.g * kRows + 16 * h;
+    float v[16][C];
+    get_rows<T, C, 16>(dy + r0 * ldd + b.c, ldd, left - 16 * h, b.n, v);
+    T* dst = dz + r0 * cols + b.c;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (ACT != kActNone) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) v[i][c] *= act_slope(q8_value(code_at(&w[c][h], i), s[c]), ACT);
+      }
+      if (16 * h + i < left) {
+        if (ACT != kActNone) set<T, C>(dst + i * cols, b.n, v[i]);
+#pragma unroll
+        for (int c = 0; c < C; ++c) sum[c] += v[i][c];
+      }
+    }
   }
-  if (part) part[at] = sum;
+  if (part)
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (c < b.n) part[at + c] = sum[c];
 }
 
+// The groups' sums of a column, in 64 bits and a fixed order: 16 threads take
+// every 16th group each, one adds them.
 template <class T>
-__global__ void dbias_kernel(const float* __restrict__ part, int64_t groups, int64_t cols, T* __restrict__ out) {
-  const int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (c >= cols) return;
+__global__ __launch_bounds__(1024) void dbias_kernel(const float* __restrict__ part, int64_t groups, int64_t cols,
+                                                     T* __restrict__ out) {
+  __shared__ double sums[16][64];
+  const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
   double s = 0.;
-  for (int64_t g = 0; g < groups; ++g) s += (double)part[g * cols + c];
-  out[c] = (T)(float)s;
+  if (c < cols)
+    for (int64_t g = row; g < groups; g += 16) s += (double)part[g * cols + c];
+  sums[row][lane] = s;
+  __syncthreads();
+  if (row == 0 && c < cols) {
+    for (int r = 1; r < 16; ++r) s += sums[r][lane];
+    out[c] = (T)(float)s;
+  }
 }
 
 // ---------------------------------------------------------------- trellis codes
