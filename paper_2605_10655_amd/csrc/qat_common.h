@@ -72,6 +72,24 @@ __device__ __forceinline__ int q8_code(float v, const Q8& q) {
   return (int)fminf(fmaxf(rintf(v * q.inv), -q.top), q.top);
 }
 
+// Whether a group whose largest magnitude has these bits is finite and below
+// the codes' cut at 63: then no value needs a bound of its own, as |v| <= 127 *
+// 2^e.
+__device__ __forceinline__ bool q8_plain(uint32_t top, int emax) {
+  return top < 0x7f800000u && (int)((top + 0x1ffffu) >> 23) - 133 < emax;
+}
+
+// Four codes of such a group: v / 2^e is exact, and added to 1.5 * 2^23 it is
+// rounded half to even into the low bits.
+__device__ __forceinline__ uint32_t q8_codes4(float a, float b, float c, float d, float inv) {
+  const float m = 12582912.f;
+  const uint32_t x = __float_as_uint(__builtin_fmaf(a, inv, m)), y = __float_as_uint(__builtin_fmaf(b, inv, m));
+  const uint32_t z = __float_as_uint(__builtin_fmaf(c, inv, m)), w = __float_as_uint(__builtin_fmaf(d, inv, m));
+  // bytes 0 of both operands side by side, then the two halves
+  const uint32_t lo = __builtin_amdgcn_perm(y, x, 0x0c0c0400u), hi = __builtin_amdgcn_perm(w, z, 0x04000c0cu);
+  return lo | hi;
+}
+
 // the scale's bf16 bits; negative where the group holds a non-finite value
 __device__ __forceinline__ uint16_t q8_scale_bits(const Q8& q, bool bad) {
   return (uint16_t)(((uint32_t)(q.e + 127) << 7) | (bad ? 0x8000u : 0u));

@@ -62,29 +62,35 @@ __device__ __forceinline__ void to_lds16(const void* g, void* lds) {
 }
 
 // ---------------------------------------------------------------- one operand's tile
-// R rows x 128 bytes of k (kStep values), in units of 16 bytes ("chunks").
-//   row, codes: place(r, c) = 8 r + (c ^ (r & 7)): a read takes one chunk of
-//     each of 32 consecutive rows, and the exclusive or spreads those over
-//     all banks.
+// R rows x 128 bytes of k (kStep values; whole cache lines: with 64 bytes the
+// copies alone took 1.4 times as long), in units of 16 bytes ("chunks").
+//   row, codes: place(r, c) = 8 r + (c ^ (r / 2 & 7)): a read takes one chunk
+//     of each of 32 consecutive rows; with the exclusive or any 16 of them that
+//     are served together lie in the 256 bytes of all banks (with r & 7 in its
+//     place they met in half of them: 0.46 of the LDS cycles were conflicts).
 //   col, 16 bits: [k][R], chunk c of k's row at c ^ swizzle(k): the transposed
 //     read takes 64 bytes of each of 8 k, which then lie in different banks.
 //   col, 32 bits: [k][R] as it is: a read takes 32 consecutive rows of one k.
-template <class T, int MODE, int R, int THREADS>
+//
+// The tile's row l is the operand's row r0 + (l / RUN) * STRIDE + l % RUN.
+template <class T, int MODE, int R, int THREADS, int RUN = R, int STRIDE = R>
 struct Tile {
   static constexpr int E = kPer16<T>;
-  static constexpr int kStep = 8 * E;                   // k of a tile
-  static constexpr int kChunks = R * 8;                 // 16-byte chunks
+  static constexpr int kRowChunks = 8;
+  static constexpr int kStep = kRowChunks * E;          // k of a tile
+  static constexpr int kChunks = R * kRowChunks;        // 16-byte chunks
   static constexpr int kPer = kChunks / THREADS;        // of them per thread
-  static constexpr int kLine = MODE == kCol ? R / E : 8;  // chunks of an LDS line
-  static constexpr int kCodeRuns = R * kStep / 16;      // 16-byte runs of codes
-  static constexpr int kLoads = (kCodeRuns + THREADS - 1) / THREADS;
+  static constexpr int kLine = MODE == kCol ? R / E : kRowChunks;  // chunks of an LDS line
+  static constexpr int kRuns = kStep / 16;              // 16-byte runs of codes in a row
+  static constexpr int kLoads = (R * kRuns + THREADS - 1) / THREADS;
   using V = typename Vec<T>::type;
 
   static __device__ __forceinline__ int swizzle(int line) {
-    if (MODE != kCol) return line & 7;
+    if (MODE != kCol) return (line >> 1) & 7;
     if (sizeof(T) == 4) return 0;
     return R >= 128 ? (line & 3) << 2 : ((line >> 1) & 1) << 2;
   }
+  static __device__ __forceinline__ int row_of(int l) { return l / RUN * STRIDE + l % RUN; }
   static __device__ __forceinline__ int place(int line, int c) { return line * kLine + (c ^ swizzle(line)); }
 
   // Asynchronous copy of k0 .. k0 + kStep - 1 into LDS, straight from memory:
@@ -103,63 +109,77 @@ struct Tile {
   static __device__ __forceinline__ void start(Copy& s, const void* p, int64_t ld, int64_t rows, int64_t r0,
                                                int64_t k0, int tid) {
     const uint32_t ldb = (uint32_t)(ld * (int64_t)sizeof(T));
-    const int last = (int)(rows - r0 < R ? rows - r0 : R);   // rows of this tile
+    const int span = R / RUN * STRIDE;
+    const int last = (int)(rows - r0 < span ? rows - r0 : span);   // rows from r0 on
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int at = i * THREADS + tid;
       const int line = at / kLine, c = (at % kLine) ^ swizzle(line);
-      if (MODE == kRow)
-        s.off[i] = (uint32_t)(line < last ? line : last - 1) * ldb + c * 16;
-      else
-        s.off[i] = (uint32_t)line * ldb + (c * E < last ? c * 16 : (last - E) * (int)sizeof(T));
+      if (MODE == kRow) {
+        const int r = row_of(line);
+        s.off[i] = (uint32_t)(r < last ? r : last - 1) * ldb + c * 16;
+      } else {
+        const int r = row_of(c * E);
+        s.off[i] = (uint32_t)line * ldb + (r < last ? r : last - E) * (int)sizeof(T);
+      }
     }
     const int64_t first = MODE == kRow ? r0 * ld + k0 : k0 * ld + r0;
     s.base = static_cast<const char*>(p) + first * (int64_t)sizeof(T);
     s.step = (MODE == kRow ? kStep : kStep * ld) * (int64_t)sizeof(T);
   }
 
-  static __device__ __forceinline__ void copy(Copy& s, int64_t k_left, V* lds, int tid) {
-    const int wave = tid >> 6;
-    if (k_left >= kStep) {
+  // A whole step.  The tile's start (a buffer resource) and the LDS places are
+  // uniform: a load costs no vector instruction.  The caller moves base on.
+  static __device__ __forceinline__ void copy(const Copy& s, V* lds, int tid) {
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(s.base), 0, 0x7fffffff, 0x00020000);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) to_lds16(s.base + s.off[i], lds + i * THREADS + wave * 64);
-    } else {
+    for (int i = 0; i < kPer; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          r, (__attribute__((address_space(3))) void*)(lds + i * THREADS + wave * 64), 16, (int)s.off[i], 0, 0, 0);
+  }
+
+  // The ragged end of k from k0 on.
+  static __device__ __forceinline__ void copy_rest(const void* p, int64_t ld, int64_t rows, int64_t K, int64_t r0,
+                                                   int64_t k0, V* lds, int tid) {
+    Copy s;
+    start(s, p, ld, rows, r0, k0, tid);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int at = i * THREADS + tid, line = at / kLine;
-        const int k = MODE == kRow ? ((at % kLine) ^ swizzle(line)) * E : line;
-        const char* src = s.base + s.off[i];
-        if (k >= k_left) src = reinterpret_cast<const char*>(kZeros);
-        to_lds16(src, lds + i * THREADS + wave * 64);
-      }
+    for (int i = 0; i < kPer; ++i) {
+      const int at = i * THREADS + tid, line = at / kLine;
+      const int k = MODE == kRow ? ((at % kLine) ^ swizzle(line)) * E : line;
+      const char* src = k0 + k < K ? s.base + s.off[i] : reinterpret_cast<const char*>(kZeros);
+      to_lds16(src, lds + i * THREADS + wave * 64);
     }
-    s.base += s.step;
   }
 
   // The same through registers, for any alignment: whole chunks by one load
   // (which need not be aligned), those that cross an edge by value.
   struct Regs {
-    V v[kPer];
-    uint16_t s[kPer];
+    V v[MODE == kCodes ? kLoads : kPer];
+    uint16_t s[MODE == kCodes ? kLoads : 1];
   };
 
   static __device__ __forceinline__ void fetch(const void* p, int64_t ld, const uint16_t* scales, int64_t rows,
                                                int64_t K, int64_t r0, int64_t k0, Regs& g, int tid) {
     if (MODE == kCodes) {
-      // 16 codes a load; consecutive threads along a group's 32, then rows
+      // 16 codes a load, a row's runs by neighbouring threads.  Every thread
+      // loads, those past the tile its first run again: the number of loads
+      // under way is then the same in every wave.
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int at = i * THREADS + tid;
-        if (kCodeRuns % THREADS && at >= kCodeRuns) break;
-        const int64_t grp = k0 / kRows + at / (2 * R);
-        int64_t r = r0 + (at >> 1) % R;
+        const int at = (i * THREADS + tid) % (R * kRuns);
+        const int64_t k = k0 + at % kRuns * 16, grp = k / kRows;
+        int64_t r = r0 + at / kRuns;
         r = r < rows ? r : rows - 1;
-        const bool in = grp * kRows < K;
+        const bool in = k < K;
         const int64_t o = in ? grp * rows + r : 0;
-        u32x4 q = *reinterpret_cast<const u32x4*>(static_cast<const int8_t*>(p) + o * kRows + (at & 1) * 16);
+        u32x4 q = *reinterpret_cast<const u32x4*>(static_cast<const int8_t*>(p) + o * kRows + (in ? k % kRows : 0));
         if (!in) q = u32x4{0, 0, 0, 0};
         __builtin_memcpy(&g.v[i], &q, 16);
-        g.s[i] = in ? scales[o] : (uint16_t)0;
+        g.s[i] = scales[o];
       }
       return;
     }
@@ -186,26 +206,70 @@ struct Tile {
     }
   }
 
+  // Codes of whole steps, one after another: offsets from the step's first
+  // group that stay the same (below 2^28 bytes), so that a load costs no
+  // vector instruction.  The caller moves the bases on.
+  struct Codes {
+    uint32_t off[kLoads], soff[kLoads];
+    const char *base, *sbase;
+    int64_t step;     // groups' rows of a step
+  };
+
+  static __device__ __forceinline__ void start_codes(Codes& c, const void* p, const uint16_t* scales, int64_t rows,
+                                                     int64_t r0, int64_t k0, int tid) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = (i * THREADS + tid) % (R * kRuns);
+      const int k = at % kRuns * 16;
+      int64_t r = r0 + at / kRuns;
+      r = r < rows ? r : rows - 1;
+      const uint32_t o = (uint32_t)(k / kRows * rows + r);
+      c.off[i] = o * kRows + k % kRows;
+      c.soff[i] = o * 2;
+    }
+    c.base = static_cast<const char*>(p) + k0 * rows;
+    c.sbase = reinterpret_cast<const char*>(scales + k0 / kRows * rows);
+    c.step = kStep / kRows * rows;
+  }
+
+  static __device__ __forceinline__ void fetch_all(const Codes& c, Regs& g) {
+    const __amdgpu_buffer_rsrc_t q =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(c.base), 0, 0x7fffffff, 0x00020000);
+    const __amdgpu_buffer_rsrc_t s =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(c.sbase), 0, 0x7fffffff, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(q, (int)c.off[i], 0, 0);
+      __builtin_memcpy(&g.v[i], &v, 16);
+      g.s[i] = __builtin_amdgcn_raw_buffer_load_b16(s, (int)c.soff[i], 0, 0);
+    }
+  }
+
   static __device__ __forceinline__ void put(const Regs& g, V* lds, int tid) {
     if (MODE == kCodes) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int at = i * THREADS + tid;
-        if (kCodeRuns % THREADS && at >= kCodeRuns) break;
-        const int r = (at >> 1) % R, c0 = (at / (2 * R)) * (kRows / E) + (at & 1) * (16 / E);
+        if (R * kRuns % THREADS && at >= R * kRuns) break;
+        const int r = at / kRuns, c0 = at % kRuns * (16 / E);
         // a group with a non-finite value counts as NaN whole: its column of
         // the gradient is not finite in either case
         const uint16_t s = g.s[i];
         const float f = (s & 0x8000u) ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)s << 16);
         uint32_t q[4];
         __builtin_memcpy(q, &g.v[i], 16);
+        // codes + 128 are bytes, which convert in one instruction; the
+        // products and their difference are exact
+        const float shift = -128.f * f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) q[w] ^= 0x80808080u;
 #pragma unroll
         for (int u = 0; u < 16 / E; ++u) {
           V v;
 #pragma unroll
           for (int e = 0; e < E; ++e) {
             const int j = u * E + e;
-            v[e] = (T)((float)((int)(q[j >> 2] << (24 - 8 * (j & 3))) >> 24) * f);
+            v[e] = (T)__builtin_fmaf((float)((q[j >> 2] >> (8 * (j & 3))) & 255u), f, shift);
           }
           lds[place(r, c0 + u)] = v;
         }
@@ -247,6 +311,26 @@ struct Tile {
 };
 
 // ---------------------------------------------------------------- epilogue
+// Waits until at most N of this wave's loads are under way.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  static_assert(N < 64, "six bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+  asm volatile("" ::: "memory");
+}
+
+// A workgroup barrier that leaves loads under way: this wave's LDS reads and
+// writes are done, and none moves across it.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);   // LDS
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+
 // LDS written by some lanes of a wave is read by others
 __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -264,30 +348,56 @@ __device__ __forceinline__ void checkpoint_strip(int8_t* codes, uint16_t* scales
   const int64_t j = j0 + col;
   const int rows = I - i0 < kRows ? (int)(I - i0) : kRows;
   const float b = bias && j < J ? (float)bias[j] : 0.f;
-  float z[kN], amax = 0.f;
-  int bad = 0;
+  float z[kN];
+  uint32_t top = 0;     // the largest magnitude's bits
 #pragma unroll
   for (int r = 0; r < kN; ++r) {
     z[r] = r0 + r < rows ? strip[(r0 + r) * (WJ + 4) + col] + b : 0.f;
-    const bool fin = finite_bits(z[r]);
-    amax = fmaxf(amax, fin ? fabsf(z[r]) : 0.f);
-    bad |= !fin;
+    const uint32_t m = __float_as_uint(z[r]) & 0x7fffffffu;
+    top = m > top ? m : top;
   }
   if (WJ == 32) {
-    amax = fmaxf(amax, __shfl_xor(amax, 32));
-    bad |= __shfl_xor(bad, 32);
+    const uint32_t m = __shfl_xor(top, 32);
+    top = m > top ? m : top;
+  }
+  const int64_t at = (i0 / kRows) * J + j;
+  uint16_t s;
+  uint32_t w[kN / 4];
+  const bool plain = q8_plain(top, kEmax<float>);
+  if (plain) {
+    const Q8 q = q8_of(__uint_as_float(top), kEmin<float>, kEmax<float>);
+#pragma unroll
+    for (int r = 0; r < kN; r += 4) w[r >> 2] = q8_codes4(z[r], z[r + 1], z[r + 2], z[r + 3], q.inv);
+    s = q8_scale_bits(q, false);
+  }
+  // (both lanes of a column agree which)
+  if (!plain) {
+    float amax = 0.f;
+    int bad = 0;
+#pragma unroll 1
+    for (int r = 0; r < kRows; ++r) {
+      const float v = r < rows ? strip[r * (WJ + 4) + col] + b : 0.f;
+      if (finite_bits(v))
+        amax = fmaxf(amax, fabsf(v));
+      else
+        bad = 1;
+    }
+    const Q8 q = q8_of(amax, kEmin<float>, kEmax<float>);
+    s = q8_scale_bits(q, bad != 0);
+    if (j < J) {
+#pragma unroll 1
+      for (int r = r0; r < r0 + kN; ++r)
+        codes[at * kRows + r] = (int8_t)q8_code(r < rows ? strip[r * (WJ + 4) + col] + b : 0.f, q);
+      if (lane < WJ) scales[at] = s;
+    }
+    return;
   }
   if (j >= J) return;
-  const Q8 q = q8_of(amax, kEmin<float>, kEmax<float>);
-  const int64_t at = (i0 / kRows) * J + j;
 #pragma unroll
-  for (int o = 0; o < kN / 16; ++o) {
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int r = 0; r < 16; ++r) w[r >> 2] |= (uint32_t)(q8_code(z[16 * o + r], q) & 255) << (8 * (r & 3));
-    *reinterpret_cast<u32x4*>(codes + at * kRows + r0 + 16 * o) = u32x4{w[0], w[1], w[2], w[3]};
-  }
-  if (lane < WJ) scales[at] = q8_scale_bits(q, bad != 0);
+  for (int o = 0; o < kN / 16; ++o)
+    *reinterpret_cast<u32x4*>(codes + at * kRows + r0 + 16 * o) =
+        u32x4{w[4 * o], w[4 * o + 1], w[4 * o + 2], w[4 * o + 3]};
+  if (lane < WJ) scales[at] = s;
 }
 
 // 32 rows x WJ columns of C from LDS: bias, activation, residual, out in runs
@@ -333,129 +443,356 @@ __device__ __forceinline__ void put_strip(T* y, int64_t ldy, const T* bias, cons
 }
 
 // ---------------------------------------------------------------- product
-// BI x BJ of C per workgroup, WI x WJ of them per wave in 32 x 32 matrix
-// instructions, 128 bytes of k a step, two LDS buffers: the next step's tiles
-// travel while this one's are multiplied.  COPY: both operands straight into
-// LDS (codes always through registers, where they become T).
-template <class T, int AM, int BM, int BI, int BJ, int WI, int WJ, bool COPY>
-__global__ __launch_bounds__((BI / WI) * (BJ / WJ) * 64) void gemm_kernel(GemmArgs g, int ti, int tj) {
-  constexpr int kThreads = (BI / WI) * (BJ / WJ) * 64;
-  constexpr int NI = WI / 32, NJ = WJ / 32;
-  using TA = Tile<T, AM, BI, kThreads>;
-  using TB = Tile<T, BM, BJ, kThreads>;
+template <int N>
+struct Half {
+  static constexpr int value = N;
+};
+
+// Consecutive workgroups go to the 8 dies in turn: each die is given a
+// contiguous run of tiles, in bands of 8 tile rows, so that its L2 holds the
+// rows of A and B that its workgroups share.
+struct Place {
+  int part, i, j;
+};
+
+__device__ __forceinline__ Place place_of(int ti, int tj, int splits) {
+  const int n = ti * tj * splits, per = n / 8, rest = n % 8, die = blockIdx.x % 8;
+  int id = die * per + (die < rest ? die : rest) + blockIdx.x / 8;
+  Place p;
+  p.part = id / (ti * tj);
+  id -= p.part * ti * tj;
+  const int band = id / (8 * tj), high = ti - band * 8 < 8 ? ti - band * 8 : 8, in = id - band * 8 * tj;
+  p.i = band * 8 + in % high;
+  p.j = in / high;
+  return p;
+}
+
+// The sums of a wave (columns lane & 31 of its 32 x 32 tiles, rows 8 (r / 4) +
+// 4 (lane / 32) + r % 4 for r = 0..15) through its strip of LDS, so that a lane
+// stores 16 bytes of one row.
+template <class T, int NI, int NJ>
+__device__ __forceinline__ void finish(const GemmArgs& g, int part, f32x16 (&acc)[NI][NJ], float* strip, int lane,
+                                       int64_t i0, int64_t j0) {
+  constexpr int WJ = 32 * NJ;
+  const T* bias = static_cast<const T*>(g.bias);
+#pragma unroll
+  for (int x = 0; x < NI; ++x) {
+    const int64_t ib = i0 + 32 * x;
+#pragma unroll
+    for (int y = 0; y < NJ; ++y)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        strip[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * (WJ + 4) + 32 * y + (lane & 31)] = acc[x][y][r];
+    wave_sync();
+    if (g.splits > 1) {
+      put_strip<float, WJ>(g.part + (int64_t)part * g.I * g.J, g.J, nullptr, nullptr, 0, kActNone, strip, lane, ib,
+                           j0, g.I, g.J);
+    } else {
+      if (g.zcodes && ib < g.I) checkpoint_strip<T, WJ>(g.zcodes, g.zscales, bias, strip, lane, ib, j0, g.I, g.J);
+      put_strip<T, WJ>(static_cast<T*>(g.y), g.ldy, bias, static_cast<const T*>(g.residual), g.ldr, g.act, strip, lane,
+                       ib, j0, g.I, g.J);
+    }
+    wave_sync();
+  }
+}
+
+// BT x BT of C per workgroup of four waves, W x W of them per wave in 32 x 32
+// matrix instructions, 128 bytes of k a step through two LDS buffers: while one
+// step is multiplied the next one's tiles travel, and the other workgroups of
+// the CU fill this one's waits.  COPY: both operands straight into LDS (codes
+// always through registers, where they become T).
+template <class T, int AM, int BM, int BT, int W, bool COPY>
+__global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
+  constexpr int kThreads = 256, NT = W / 32;
+  static_assert((BT / W) * (BT / W) == 4, "four waves");
+  using TA = Tile<T, AM, BT, kThreads>;
+  using TB = Tile<T, BM, BT, kThreads>;
   using V = typename Vec<T>::type;
   constexpr bool kCopyA = COPY && AM != kCodes, kCopyB = COPY && BM != kCodes;
   // Two buffers of their own names: the compiler then knows that a copy into
-  // one does not touch what is read from the other, and waits for neither.
-  // The epilogue's strip of a wave is 32 rows x WJ sums in the first, rows
-  // padded by 16 bytes.
-  constexpr int kLine = WJ + 4, kStrip = 32 * kLine, kStrips = kThreads / 64 * kStrip / 4;
-  constexpr int kBuf = TA::kChunks + TB::kChunks;
-  __shared__ __align__(16) V lds0[kBuf > kStrips ? kBuf : kStrips];
+  // one does not touch what is read from the other, and waits for neither.  The
+  // epilogue's strips (32 rows x W sums a wave, rows padded by 16 bytes) lie in
+  // them, half of the waves in each.
+  constexpr int kBuf = TA::kChunks + TB::kChunks, kStrip = 32 * (W + 4);
+  static_assert(2 * kStrip * 4 <= kBuf * 16, "strips fit the buffers");
+  __shared__ __align__(16) V lds0[kBuf];
   __shared__ __align__(16) V lds1[kBuf];
 
-  // Consecutive workgroups go to the 8 dies in turn: give each die a
-  // contiguous run of tiles, in bands of 8 tile rows, so that its L2 holds the
-  // rows of A and B that its workgroups share.
-  const int n = ti * tj * g.splits;
-  int id = blockIdx.x;
-  {
-    const int per = n / 8, rest = n % 8, die = id % 8, in = id / 8;
-    id = die * per + (die < rest ? die : rest) + in;
-  }
-  const int part = id / (ti * tj);
-  id -= part * ti * tj;
-  const int band = id / (8 * tj), rows_of = ti - band * 8 < 8 ? ti - band * 8 : 8, in = id - band * 8 * tj;
-  const int64_t i0 = (int64_t)(band * 8 + in % rows_of) * BI, j0 = (int64_t)(in / rows_of) * BJ;
-
+  const Place p = place_of(ti, tj, g.splits);
+  const int64_t i0 = (int64_t)p.i * BT, j0 = (int64_t)p.j * BT;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wi = (wave / (BJ / WJ)) * WI, wj = (wave % (BJ / WJ)) * WJ;
-  f32x16 acc[NI][NJ];
+  const int wi = (wave >> 1) * W, wj = (wave & 1) * W;
+  f32x16 acc[NT][NT];
 #pragma unroll
-  for (int x = 0; x < NI; ++x)
+  for (int x = 0; x < NT; ++x)
+#pragma unroll
+    for (int y = 0; y < NT; ++y)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
+
+  const int64_t all = (g.K + TA::kStep - 1) / TA::kStep;
+  const int64_t first = all * p.part / g.splits;
+  const int steps = (int)(all * (p.part + 1) / g.splits - first);
+  typename TA::Regs ra;
+  typename TB::Regs rb;
+  typename TA::Copy ca;
+  typename TB::Copy cb;
+  if constexpr (kCopyA) TA::start(ca, g.a, g.lda, g.I, i0, first * TA::kStep, tid);
+  if constexpr (kCopyB) TB::start(cb, g.b, g.ldb, g.J, j0, first * TA::kStep, tid);
+  auto copy = [&](int s, V* lds) __attribute__((always_inline)) {
+    if (s >= steps) return;
+    const int64_t k0 = (first + s) * TA::kStep;
+    if (k0 + TA::kStep <= g.K) {
+      if constexpr (kCopyA) {
+        TA::copy(ca, lds, tid);
+        ca.base += ca.step;
+      }
+      if constexpr (kCopyB) {
+        TB::copy(cb, lds + TA::kChunks, tid);
+        cb.base += cb.step;
+      }
+    } else {
+      if constexpr (kCopyA) TA::copy_rest(g.a, g.lda, g.I, g.K, i0, k0, lds, tid);
+      if constexpr (kCopyB) TB::copy_rest(g.b, g.ldb, g.J, g.K, j0, k0, lds + TA::kChunks, tid);
+    }
+  };
+  // operands through registers: one step's under way.  (The fences keep these
+  // loads younger than the copies before them.)
+  auto fetch = [&](int s) __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+    if (s >= steps) return;
+    const int64_t k0 = (first + s) * TA::kStep;
+    if constexpr (!kCopyA) TA::fetch(g.a, g.lda, nullptr, g.I, g.K, i0, k0, ra, tid);
+    if constexpr (!kCopyB) TB::fetch(g.b, g.ldb, g.bscales, g.J, g.K, j0, k0, rb, tid);
+    asm volatile("" ::: "memory");
+  };
+  auto put = [&](int s, V* lds) __attribute__((always_inline)) {
+    if (s >= steps) return;
+    if constexpr (!kCopyA) TA::put(ra, lds, tid);
+    if constexpr (!kCopyB) TB::put(rb, lds + TA::kChunks, tid);
+  };
+  auto step = [&](int s, V* now, V* other) __attribute__((always_inline)) {
+    // This step's tiles have landed (the codes of the next, loaded after its
+    // copies, may be under way), and no wave still reads the other buffer.
+    if (kCopyA && !kCopyB && s + 1 < steps)
+      wait_copies<TB::kLoads>();
+    else if (kCopyA || kCopyB)
+      wait_copies<0>();
+    lds_barrier();
+    copy(s + 1, other);
+    V fa[4][NT], fb[4][NT];
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        fa[kk][x] = TA::operand(now, wi + 32 * x, kk, lane);
+        fb[kk][x] = TB::operand(now + TA::kChunks, wj + 32 * x, kk, lane);
+      }
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int y = 0; y < NT; ++y) mma<T>(fa[kk][x], fb[kk][y], acc[x][y]);
+    put(s + 1, other);
+    fetch(s + 2);
+  };
+  if (steps > 0) {
+    fetch(0);
+    copy(0, lds0);
+    put(0, lds0);
+    fetch(1);
+  }
+  for (int s = 0; s < steps; s += 2) {
+    step(s, lds0, lds1);
+    if (s + 1 < steps) step(s + 1, lds1, lds0);
+  }
+  __syncthreads();
+  finish<T, NT, NT>(g, p.part, acc, reinterpret_cast<float*>(wave < 2 ? lds0 : lds1) + (wave & 1) * kStrip, lane,
+                    i0 + wi, j0 + wj);
+}
+
+// The same for large products: 256 x 256 of C per workgroup of eight waves, 128
+// x 64 of them per wave, A always copied.
+//
+// A step's 128 bytes of k are multiplied in two halves: first the upper 64 rows
+// of each wave's part, then the lower 64 with the operands of B kept in
+// registers.  B's tile and A's upper half tile are then free half a step before
+// A's lower one, and each is refilled at once for the step after next: every
+// copy has a step and a half to travel, at any time there are copies under way,
+// and two buffers suffice.  (With all copies started at the beginning of a step
+// and waited for at its end the copies alone took 3460 cycles a step, the
+// matrix instructions 2048.)
+//
+// A half has a reading and a multiplying turn, and the second four waves run
+// one turn behind the first: while one wave of a SIMD multiplies, the other
+// reads its operands from LDS, starts copies and turns codes into T.  The turn
+// before the first waves read a tile is a reading one of the second four's: by
+// its end every wave has seen its copies of that tile land.
+template <class T, int AM, int BM>
+__global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int tj) {
+  constexpr int kThreads = 512, BT = 256, NJ = 2;
+  using TA = Tile<T, AM, 128, kThreads, 64, 128>;   // half h: rows 64 h of every 128
+  using TB = Tile<T, BM, 256, kThreads>;
+  using V = typename Vec<T>::type;
+  constexpr bool kCopyB = BM != kCodes;
+  // tiles of their own names, as above
+  __shared__ __align__(16) V up0[TA::kChunks];
+  __shared__ __align__(16) V up1[TA::kChunks];
+  __shared__ __align__(16) V low0[TA::kChunks];
+  __shared__ __align__(16) V low1[TA::kChunks];
+  __shared__ __align__(16) V b0[TB::kChunks];
+  __shared__ __align__(16) V b1[TB::kChunks];
+  constexpr int kStrip = 32 * (64 + 4);   // 8.5 KB
+  static_assert(3 * kStrip * 4 <= TB::kChunks * 16 && kStrip * 4 <= TA::kChunks * 16, "strips fit the tiles");
+
+  const Place p = place_of(ti, tj, g.splits);
+  const int64_t i0 = (int64_t)p.i * BT, j0 = (int64_t)p.j * BT;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wi = (wave >> 2) * 128, wj = (wave & 3) * 64;
+  const bool behind = wave >= 4;
+  f32x16 acc[4][NJ];
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
 #pragma unroll
     for (int y = 0; y < NJ; ++y)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
 
-  const int64_t steps = (g.K + TA::kStep - 1) / TA::kStep;
-  const int64_t s0 = steps * part / g.splits, s1 = steps * (part + 1) / g.splits;
-  typename TA::Regs ra;
+  // Whole steps; what is left of k goes first, on its own.
+  const int64_t all = g.K / TA::kStep;
+  const int64_t first = all * p.part / g.splits;
+  const int steps = (int)(all * (p.part + 1) / g.splits - first);
+  V fa[4][2], fb[4][NJ];
+  auto read_a = [&](const V* a) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) fa[kk][x] = TA::operand(a, wi / 2 + 32 * x, kk, lane);
+  };
+  auto read_b = [&](const V* b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int y = 0; y < NJ; ++y) fb[kk][y] = TB::operand(b, wj + 32 * y, kk, lane);
+  };
+  auto multiply = [&](auto half) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int y = 0; y < NJ; ++y) mma<T>(fa[kk][x], fb[kk][y], acc[2 * decltype(half)::value + x][y]);
+    __builtin_amdgcn_s_setprio(0);
+  };
+  // (a lower half past the last row reads from the first)
+  const int64_t il = i0 + 64 < g.I ? i0 + 64 : i0;
   typename TB::Regs rb;
-  typename TA::Copy ca;
-  typename TB::Copy cb;
-  if constexpr (kCopyA) TA::start(ca, g.a, g.lda, g.I, i0, s0 * TA::kStep, tid);
-  if constexpr (kCopyB) TB::start(cb, g.b, g.ldb, g.J, j0, s0 * TA::kStep, tid);
-  auto begin = [&](int64_t s, V* lds) __attribute__((always_inline)) {
-    const int64_t k0 = s * TA::kStep;
-    if constexpr (kCopyA)
-      TA::copy(ca, g.K - k0, lds, tid);
-    else
-      TA::fetch(g.a, g.lda, nullptr, g.I, g.K, i0, k0, ra, tid);
-    if constexpr (kCopyB)
-      TB::copy(cb, g.K - k0, lds + TA::kChunks, tid);
-    else
-      TB::fetch(g.b, g.ldb, g.bscales, g.J, g.K, j0, k0, rb, tid);
-  };
-  auto end = [&](V* lds) __attribute__((always_inline)) {
-    if constexpr (!kCopyA) TA::put(ra, lds, tid);
-    if constexpr (!kCopyB) TB::put(rb, lds + TA::kChunks, tid);
-  };
-  auto step = [&](int64_t s, const V* now, V* next) __attribute__((always_inline)) {
-    // this step's tiles have landed (every wave waits for its own part), and
-    // no wave still reads the other buffer
-    __syncthreads();
-    if (s + 1 < s1) begin(s + 1, next);
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      V fa[NI], fb[NJ];
-#pragma unroll
-      for (int x = 0; x < NI; ++x) fa[x] = TA::operand(now, wi + 32 * x, kk, lane);
-#pragma unroll
-      for (int y = 0; y < NJ; ++y) fb[y] = TB::operand(now + TA::kChunks, wj + 32 * y, kk, lane);
-#pragma unroll
-      for (int x = 0; x < NI; ++x)
-#pragma unroll
-        for (int y = 0; y < NJ; ++y) mma<T>(fa[x], fb[y], acc[x][y]);
-    }
-    if (s + 1 < s1) end(next);
-  };
-
-  if (s0 < s1) {
-    begin(s0, lds0);
-    end(lds0);
-  }
-  for (int64_t s = s0; s < s1; s += 2) {
-    step(s, lds0, lds1);
-    if (s + 1 < s1) step(s + 1, lds1, lds0);
-  }
-
-  // lane: column lane & 31 of a 32 x 32 tile, rows 8 (r / 4) + 4 (lane / 32) +
-  // r % 4 for r = 0..15.  The sums go through the wave's own strip of LDS, so
-  // that a lane stores 16 bytes of one row.
-  __syncthreads();
-  float* strip = reinterpret_cast<float*>(lds0) + wave * kStrip;
-  const T* bias = static_cast<const T*>(g.bias);
-#pragma unroll
-  for (int x = 0; x < NI; ++x) {
-    const int64_t ib = i0 + wi + 32 * x;
-#pragma unroll
-    for (int y = 0; y < NJ; ++y)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        strip[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kLine + 32 * y + (lane & 31)] = acc[x][y][r];
-    wave_sync();
-    if (g.splits > 1) {
-      put_strip<float, WJ>(g.part + (int64_t)part * g.I * g.J, g.J, nullptr, nullptr, 0, kActNone, strip, lane, ib,
-                           j0 + wj, g.I, g.J);
+  if (g.K % TA::kStep && p.part == g.splits - 1) {
+    const int64_t k0 = all * TA::kStep;
+    TA::copy_rest(g.a, g.lda, g.I, g.K, i0, k0, up0, tid);
+    TA::copy_rest(g.a, g.lda, g.I, g.K, il, k0, low0, tid);
+    if constexpr (kCopyB) {
+      TB::copy_rest(g.b, g.ldb, g.J, g.K, j0, k0, b0, tid);
     } else {
-      if (g.zcodes && ib < g.I)
-        checkpoint_strip<T, WJ>(g.zcodes, g.zscales, bias, strip, lane, ib, j0 + wj, g.I, g.J);
-      put_strip<T, WJ>(static_cast<T*>(g.y), g.ldy, bias, static_cast<const T*>(g.residual), g.ldr, g.act, strip, lane,
-                       ib, j0 + wj, g.I, g.J);
+      TB::fetch(g.b, g.ldb, g.bscales, g.J, g.K, j0, k0, rb, tid);
+      TB::put(rb, b0, tid);
     }
-    wave_sync();
+    wait_copies<0>();
+    lds_barrier();
+    read_b(b0);
+    read_a(up0);
+    multiply(Half<0>());
+    read_a(low0);
+    multiply(Half<1>());
+    lds_barrier();
   }
+  if (steps > 0) {
+    typename TA::Copy cu, cl;
+    typename TB::Copy cb;
+    typename TB::Codes codes;
+    TA::start(cu, g.a, g.lda, g.I, i0, first * TA::kStep, tid);
+    TA::start(cl, g.a, g.lda, g.I, il, first * TA::kStep, tid);
+    if constexpr (kCopyB)
+      TB::start(cb, g.b, g.ldb, g.J, j0, first * TA::kStep, tid);
+    else
+      TB::start_codes(codes, g.b, g.bscales, g.J, j0, first * TA::kStep, tid);
+    // Copies of step s; past the last they fetch that one again, into tiles
+    // that nothing reads any more, so that no turn has a branch (with branches
+    // for the end in it a step took 3200 cycles, without them 2360).
+    auto copy_upper = [&](int s, V* up, V* b) __attribute__((always_inline)) {
+      if constexpr (kCopyB) {
+        TB::copy(cb, b, tid);
+        cb.base += s + 1 < steps ? cb.step : 0;
+      }
+      TA::copy(cu, up, tid);
+      cu.base += s + 1 < steps ? cu.step : 0;
+    };
+    auto copy_lower = [&](int s, V* lo) __attribute__((always_inline)) {
+      TA::copy(cl, lo, tid);
+      cl.base += s + 1 < steps ? cl.step : 0;
+    };
+    // Codes: one step's under way.  (The fences keep their loads younger than
+    // the copies before them.)
+    auto fetch = [&](int s) __attribute__((always_inline)) {
+      if constexpr (!kCopyB) {
+        asm volatile("" ::: "memory");
+        TB::fetch_all(codes, rb);
+        asm volatile("" ::: "memory");
+        codes.base += s + 1 < steps ? codes.step * kRows : 0;
+        codes.sbase += s + 1 < steps ? codes.step * 2 : 0;
+      }
+    };
+    auto put = [&](V* b) __attribute__((always_inline)) {
+      if constexpr (!kCopyB) TB::put(rb, b, tid);
+    };
+    // What may be under way when the next turn's tiles have landed: all of one
+    // step's copies and one step's codes.
+    constexpr int kNew = 2 * TA::kPer + (kCopyB ? TB::kPer : TB::kLoads);
+    // Step s in the tiles up, lo, b; the other parity's are lo2 and b2.
+    auto step = [&](int s, V* up, V* lo, V* b, V* lo2, V* b2) __attribute__((always_inline)) {
+      read_b(b);
+      read_a(up);
+      // step s - 1's lower half has been read by every wave
+      copy_lower(s + 1, lo2);
+      wait_copies<kNew>();
+      lds_barrier();
+      multiply(Half<0>());
+      lds_barrier();
+      // this step's B and upper half have
+      copy_upper(s + 2, up, b);
+      put(b2);
+      fetch(s + 2);
+      read_a(lo);
+      wait_copies<kNew>();
+      lds_barrier();
+      multiply(Half<1>());
+      lds_barrier();
+    };
+    fetch(0);
+    put(b0);
+    copy_upper(0, up0, b0);
+    copy_lower(0, low0);
+    copy_upper(1, up1, b1);
+    fetch(1);
+    wait_copies<kNew>();
+    lds_barrier();
+    if (behind) lds_barrier();
+#pragma unroll 1
+    for (int s = 0; s < steps; s += 2) {
+      step(s, up0, low0, b0, low1, b1);
+      if (s + 1 == steps) break;
+      step(s + 1, up1, low1, b1, low0, b0);
+    }
+    if (!behind) lds_barrier();
+    wait_copies<0>();
+  }
+  __syncthreads();
+  // strips: three in each tile of B, one in each of two of A's
+  V* const in = wave < 3 ? b0 : wave < 6 ? b1 : wave == 6 ? up0 : up1;
+  finish<T, 4, NJ>(g, p.part, acc, reinterpret_cast<float*>(in) + (wave < 6 ? wave % 3 : 0) * kStrip, lane, i0 + wi,
+                   j0 + wj);
 }
 
 // The epilogue of a product whose k was split: the parts' sum (always in the

@@ -51,10 +51,10 @@ inline GemmPlan gemm_plan(int dtype, int64_t I, int64_t J, int64_t K) {
   return p;
 }
 
-template <class T, int AM, int BM, int BT, int WI, int WJ, bool COPY>
+template <class T, int AM, int BM, int BT, bool COPY>
 void launch_gemm(const GemmArgs& g, const GemmPlan& p, hipStream_t stream) {
-  hipLaunchKernelGGL((gemm_kernel<T, AM, BM, BT, BT, WI, WJ, COPY>), dim3((unsigned)(p.ti * p.tj * p.splits)),
-                     dim3(BT / WI * (BT / WJ) * 64), 0, stream, g, p.ti, p.tj);
+  hipLaunchKernelGGL((gemm_kernel<T, AM, BM, BT, BT / 2, COPY>), dim3((unsigned)(p.ti * p.tj * p.splits)), dim3(256),
+                     0, stream, g, p.ti, p.tj);
 }
 
 // whether tiles of an operand can be copied straight into LDS (Tile::copy)
@@ -75,16 +75,22 @@ int gemm(GemmArgs g, void* ws, hipStream_t stream) {
   g.splits = p.splits;
   g.part = static_cast<float*>(ws);
   if (copies(AM, g.a, g.lda, g.I, g.K, es, p.tile) && copies(BM, g.b, g.ldb, g.J, g.K, es, p.tile)) {
-    if (p.tile == 256) launch_gemm<T, AM, BM, 256, 128, 64, true>(g, p, stream);
-    else if (p.tile == 128) launch_gemm<T, AM, BM, 128, 64, 64, true>(g, p, stream);
-    else launch_gemm<T, AM, BM, 64, 32, 32, true>(g, p, stream);
+    if (p.tile == 256)
+      hipLaunchKernelGGL((gemm_large_kernel<T, AM, BM>), dim3((unsigned)(p.ti * p.tj * p.splits)), dim3(512), 0, stream,
+                         g, p.ti, p.tj);
+    else if (p.tile == 128)
+      launch_gemm<T, AM, BM, 128, true>(g, p, stream);
+    else
+      launch_gemm<T, AM, BM, 64, true>(g, p, stream);
   } else {
-    if (p.tile == 256) {   // both tiles through registers do not fit them (k is not split here)
+    if (p.tile == 256) {   // the large kernel copies A (k is not split here)
       p.ti = (int)ceil_div(g.I, 128);
       p.tj = (int)ceil_div(g.J, 128);
     }
-    if (p.tile >= 128) launch_gemm<T, AM, BM, 128, 64, 64, false>(g, p, stream);
-    else launch_gemm<T, AM, BM, 64, 32, 32, false>(g, p, stream);
+    if (p.tile >= 128)
+      launch_gemm<T, AM, BM, 128, false>(g, p, stream);
+    else
+      launch_gemm<T, AM, BM, 64, false>(g, p, stream);
   }
   if (launched() != BCJR_OK) return BCJR_ERR_HIP;
   if (p.splits > 1) {

@@ -67,11 +67,15 @@ __device__ __forceinline__ void get_rows(const T* p, int64_t ld, int left, int n
 #pragma unroll
       for (int c = 0; c < C; ++c) v[i][c] = (float)t[i][c];
   } else {
+    // rows past the last read the last one (left - 1 from p, below 0 for the
+    // second half of a band that ends in the first)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+      const int r = i < left ? i : left - 1;
+      float t[C];
+      get<T, C>(p + (int64_t)r * ld, n, t);
 #pragma unroll
-      for (int c = 0; c < C; ++c) v[i][c] = 0.f;
-      if (i < left) get<T, C>(p + i * ld, n, v[i]);
+      for (int c = 0; c < C; ++c) v[i][c] = i < left ? t[c] : 0.f;
     }
   }
 }
@@ -88,33 +92,50 @@ __global__ __launch_bounds__(kGroupThreads) void act8_store_kernel(const T* __re
   constexpr int C = kCols<T>;
   const Band b = band_of<C>(cols);
   if (b.n == 0) return;
-  float v[kRows][C], amax[C] = {};
-  bool bad[C] = {};
+  float v[kRows][C];
   const T* src = x + b.g * kRows * ldx + b.c;
   const int left = rows - b.g * kRows < kRows ? (int)(rows - b.g * kRows) : kRows;
   get_rows<T, C, kRows>(src, ldx, left, b.n, v);
-#pragma unroll
-  for (int i = 0; i < kRows; ++i)
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const bool fin = finite_bits(v[i][c]);
-      amax[c] = fmaxf(amax[c], fin ? fabsf(v[i][c]) : 0.f);
-      bad[c] |= !fin;
-    }
   const int64_t at = b.g * cols + b.c;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    if (c >= b.n) break;
-    const Q8 q = q8_of(amax[c], kEmin<T>, kEmax<T>);
-    u32x4* o = reinterpret_cast<u32x4*>(codes + (at + c) * kRows);
+    if (c < b.n) {
+      u32x4* o = reinterpret_cast<u32x4*>(codes + (at + c) * kRows);
+      uint32_t top = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      u32x4 w = {0, 0, 0, 0};
+      for (int i = 0; i < kRows; ++i) {
+        const uint32_t m = __float_as_uint(v[i][c]) & 0x7fffffffu;
+        top = m > top ? m : top;
+      }
+      uint32_t w[8];
+      if (q8_plain(top, kEmax<T>)) {
+        const Q8 q = q8_of(__uint_as_float(top), kEmin<T>, kEmax<T>);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) w[i >> 2] |= (uint32_t)(q8_code(v[16 * h + i][c], q) & 255) << (8 * (i & 3));
-      o[h] = w;
+        for (int i = 0; i < 8; ++i)
+          w[i] = q8_codes4(v[4 * i][c], v[4 * i + 1][c], v[4 * i + 2][c], v[4 * i + 3][c], q.inv);
+        scales[at + c] = q8_scale_bits(q, false);
+      } else {
+        // rare: the values are read again, so that this costs no registers
+        float amax = 0.f;
+        bool bad = false;
+#pragma unroll 1
+        for (int i = 0; i < left; ++i) {
+          const float f = (float)src[i * ldx + c];
+          if (finite_bits(f))
+            amax = fmaxf(amax, fabsf(f));
+          else
+            bad = true;
+        }
+        const Q8 q = q8_of(amax, kEmin<T>, kEmax<T>);
+#pragma unroll 1
+        for (int i = 0; i < kRows; ++i)
+          codes[(at + c) * kRows + i] = (int8_t)(i < left ? q8_code((float)src[i * ldx + c], q) : 0);
+        scales[at + c] = q8_scale_bits(q, bad);
+        continue;
+      }
+      o[0] = u32x4{w[0], w[1], w[2], w[3]};
+      o[1] = u32x4{w[4], w[5], w[6], w[7]};
     }
-    scales[at + c] = q8_scale_bits(q, bad[c]);
   }
 }
 
