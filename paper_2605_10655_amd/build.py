@@ -2,13 +2,14 @@
 C ABI of include/bcjr.h) and libissue_rates.so (the VALU issue-rate probe
 the benchmark prices its roofline with).
 
-libbcjr.so links seven translation units, compiled side by side:
+libbcjr.so links eight translation units, compiled side by side:
 bcjr_capi.hip (the C ABI and most kernel families), bcjr_rot.hip (the
 rotating-exchange kernels of S = 65536, k = 2), which is compiled with the
 AMDGPU max-ilp instruction scheduler, bcjr_lin.hip (the linear-domain
 kernels of the smaller trellises), qat_linear.hip (the quantised linear
-layer) and qat_gemm_{bf16,f16,f32}.hip (its matrix products, one type each);
-each object carries its own code object."""
+layer), qat_codes.hip (a few tokens through trellis-coded weights) and
+qat_gemm_{bf16,f16,f32}.hip (the layer's matrix products, one type each); each
+object carries its own code object."""
 from __future__ import annotations
 
 import os
@@ -27,7 +28,8 @@ LIB = os.path.join(PKG, "libbcjr.so")
 UNITS = [(os.path.join(CSRC, "bcjr_capi.hip"), []),
          (os.path.join(CSRC, "bcjr_rot.hip"), ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]),
          (os.path.join(CSRC, "bcjr_lin.hip"), []),
-         (os.path.join(CSRC, "qat_linear.hip"), [])] + [
+         (os.path.join(CSRC, "qat_linear.hip"), []),
+         (os.path.join(CSRC, "qat_codes.hip"), [])] + [
          (os.path.join(CSRC, f"qat_gemm_{t}.hip"), []) for t in ("bf16", "f16", "f32")]
 SOURCES = [u[0] for u in UNITS]
 RATES_SRC = os.path.join(CSRC, "issue_rates.hip")
@@ -36,6 +38,7 @@ DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in (
     "bcjr_device.h", "bcjr_kernels.h", "bcjr_vec_kernels.h", "bcjr_qat.h", "bcjr_internal.h",
     "bcjr_generic_kernels.h", "bcjr_ldlq_kernels.h", "bcjr_rot_kernels.h", "bcjr_pruned_kernels.h",
     "bcjr_lin_kernels.h", "qat_common.h", "qat_linear_kernels.h",
+    "qat_codes_kernels.h",
     "qat_gemm_kernels.h", "qat_gemm_launch.h")] + [
     os.path.join(INCLUDE, "bcjr.h")]
 

@@ -1,0 +1,253 @@
+// qat_codes_kernels.h -- a few tokens through trellis-coded weights: the bit
+// strings are turned into operands of the matrix instructions as they are read.
+#pragma once
+#include "qat_common.h"
+
+namespace bcjr {
+namespace qlin {
+
+struct CodesArgs {
+  const void* x;
+  int64_t ldx;
+  const uint32_t* packed;
+  const float* codebook;
+  const float* scales;       // [N, K / block] or null
+  const void* bias;
+  const void* residual;
+  int64_t ldr;
+  void* y;
+  int64_t ldy;
+  int act, n;
+  int M, N, K, block, words;
+  int tiles;                 // tiles of rows
+  int parts, rows_at_once;   // waves along K and along tiles
+};
+
+// y = act(x W^T + bias) + residual for up to 16 MT tokens.
+//
+// The codebook lies in LDS as T, V values a state, so that a step costs a
+// funnel shift, a shift, an address and one LDS read.  Those reads meet random
+// banks (64 lanes take 8.4 cycles) and are what bounds the kernel, not memory
+// (2 bits a weight) nor the matrix instructions; a lane's weights are therefore
+// decoded once and multiplied with all tokens.  A codebook of more than 128 KB
+// (V = 2 or fp32 at 16 state bits) is taken in parts of that size: in each, the
+// states of the others read a zero, all the same one, which costs no bank.
+//
+// A wave takes 16 / Q rows and 256 Q weights of each.  Lane l of a matrix
+// instruction holds row l % 16 and eight k; which k is free, so lane group l /
+// 16 takes 64 weights in a row, whose windows start at a word of the string.
+// With Q = 2 (at most 8 tokens) rows 8..15 are the same rows at the next 256
+// weights, tokens 8..15 the same tokens there: the products of unlike halves
+// are not used, and half the rows a tile fill twice the CUs.
+//
+// Waves of a workgroup split K; their sums meet in LDS in a fixed order.
+template <class T>
+struct Frag;   // eight weights or activations of a lane
+template <>
+struct Frag<bf16> {
+  typedef bf16 type __attribute__((ext_vector_type(8)));
+};
+template <>
+struct Frag<f16> {
+  typedef f16 type __attribute__((ext_vector_type(8)));
+};
+template <>
+struct Frag<float> {
+  typedef float type __attribute__((ext_vector_type(8)));
+};
+
+__device__ __forceinline__ void mma16(const Frag<bf16>::type& a, const Frag<bf16>::type& b, f32x4& c) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma16(const Frag<f16>::type& a, const Frag<f16>::type& b, f32x4& c) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma16(const Frag<float>::type& a, const Frag<float>::type& b, f32x4& c) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+}
+
+constexpr int kChunk = 256;       // weights of a row that a wave takes at once
+constexpr int kCodesWaves = 16;
+
+
+// State bits of a part of the codebook: 128 KB
+template <class T, int V>
+constexpr int kTableBits = sizeof(T) * V == 2 ? 16 : sizeof(T) * V == 4 ? 15 : 14;
+
+// LDS bytes: the codebook's part and a zero entry (16 bytes), then 16 x 16 sums
+// a wave
+template <class T, int V>
+constexpr size_t codes_table(int n) {
+  return (((size_t)sizeof(T) * V) << (n < kTableBits<T, V> ? n : kTableBits<T, V>)) / 16 * 16 + 32;
+}
+
+// Part h of the codebook as T, four values at a time.
+template <class T, int V>
+__device__ __forceinline__ void fill_table(T* table, const float* codebook, int n, int h, int tid, int threads) {
+  const int count = V << (n < kTableBits<T, V> ? n : kTableBits<T, V>);
+  codebook += (int64_t)h * count;
+  if (tid < V) table[count + tid] = (T)0.f;   // what states of other parts read
+  if (count < 4) {
+    if (tid < count) table[tid] = (T)codebook[tid];
+    return;
+  }
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  const f32x4* src = reinterpret_cast<const f32x4*>(codebook);
+  T4* dst = reinterpret_cast<T4*>(table);
+#pragma unroll 8
+  for (int s = tid; s < count / 4; s += threads) {
+    const f32x4 c = src[s];
+    T4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (T)c[i];
+    dst[s] = v;
+  }
+}
+
+template <class T, int KB, int V, int MT, int Q>
+__global__ __launch_bounds__(64 * kCodesWaves) void codes_kernel(CodesArgs a) {
+  using F = typename Frag<T>::type;
+  struct Entry {
+    T v[V];
+  };
+  constexpr int kRowsOf = 16 / Q;
+  constexpr int kSteps = 64 / V;                              // steps of a lane's 64 weights
+  constexpr int kWords = ((kSteps - 1) * KB + 16 + 31) / 32;  // words that they span (16 state bits)
+  extern __shared__ __align__(16) char lds[];
+  Entry* table = reinterpret_cast<Entry*>(lds);
+  float* sums = reinterpret_cast<float*>(lds + codes_table<T, V>(a.n));
+  const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 63, wave = tid >> 6;
+  const int part = wave % a.parts, of = wave / a.parts;
+  const int row = lane & 15, g = lane >> 4;
+  const int units = (a.K / kChunk + Q - 1) / Q;               // along K
+  const int pieces = a.n > kTableBits<T, V> ? 1 << (a.n - kTableBits<T, V>) : 1;
+  const int right = 32 - a.n;
+  const T* x = static_cast<const T*>(a.x);
+  const T* bias = static_cast<const T*>(a.bias);
+  const T* res = static_cast<const T*>(a.residual);
+  T* y = static_cast<T*>(a.y);
+
+  // the words of this lane's 64 weights of its row in unit u
+  auto words = [&](int tile, int u, uint32_t* w) __attribute__((always_inline)) {
+    int r = tile * kRowsOf + row % kRowsOf;
+    r = r < a.N ? r : a.N - 1;
+    int at = (u * Q + row / kRowsOf) * kChunk;                // first weight of the chunk
+    at = at < a.K ? at : 0;
+    const int64_t path = (int64_t)r * (a.K / a.block) + at / a.block;
+    const int word = (at % a.block + 64 * g) / V * KB / 32;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = a.packed[path * a.words + (word + i < a.words ? word + i : a.words - 1)];
+  };
+
+  // a token's activations at eight of this lane's weights in unit u
+  auto tokens = [&](int u, int m, int f) __attribute__((always_inline)) {
+    int tok = Q == 2 ? lane & 7 : 16 * m + row;
+    tok = tok < a.M ? tok : a.M - 1;
+    const int from = (u * Q + (Q == 2 ? row >> 3 : 0)) * kChunk;   // of the token's half
+    F xf;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) xf[e] = (T)0.f;                    // none past the end of K
+    if (Q == 1 || from < a.K) __builtin_memcpy(&xf, x + tok * a.ldx + from + 64 * g + 8 * f, sizeof(xf));
+    return xf;
+  };
+  // the scales of the sums' rows 4 g + i (and of the half that those belong to)
+  auto scales = [&](int tile, int u) __attribute__((always_inline)) {
+    f32x4 sc = {1.f, 1.f, 1.f, 1.f};
+    if (a.scales) {
+      int ch = u * Q + 4 * g / kRowsOf;
+      ch = ch * kChunk < a.K ? ch : 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        int r = tile * kRowsOf + (4 * g + i) % kRowsOf;
+        r = r < a.N ? r : a.N - 1;
+        sc[i] = a.scales[(int64_t)r * (a.K / a.block) + ch * kChunk / a.block];
+      }
+    }
+    return sc;
+  };
+
+  bool filled = false;
+  for (int t0 = blockIdx.x * a.rows_at_once; t0 < a.tiles; t0 += gridDim.x * a.rows_at_once) {
+    const int tile = t0 + of;
+    const bool live = tile < a.tiles;
+    f32x4 acc[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int h = 0; h < pieces; ++h) {
+      // the first unit's words travel while the table is filled (its scales and
+      // tokens too would leave the wave too few registers: 13.9 against 11.5 us)
+      uint32_t w[kWords];
+      if (live && part < units) words(tile, part, w);
+      if (!filled || pieces > 1) {   // (a single piece stays)
+        __syncthreads();
+        fill_table<T, V>(reinterpret_cast<T*>(table), a.codebook, a.n, h, tid, threads);
+        __syncthreads();
+        filled = true;
+      }
+      const uint32_t before = (uint32_t)h << kTableBits<T, V>, none = 1u << kTableBits<T, V>;
+      if (live)
+#pragma unroll 1
+        for (int u = part; u < units; u += a.parts) {
+          const f32x4 sc = scales(tile, u);
+          f32x4 now[MT];
+#pragma unroll
+          for (int m = 0; m < MT; ++m) now[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int f = 0; f < 8; ++f) {
+            F wf;
+#pragma unroll
+            for (int e = 0; e < 8 / V; ++e) {
+              // the n bits at bit KB * step of the string
+              const int off = KB * (8 / V * f + e), j = off >> 5, o = off & 31;
+              const uint32_t top = o == 0 ? w[j] : __builtin_amdgcn_alignbit(w[j], w[j + 1 < kWords ? j + 1 : j], 32 - o);
+              uint32_t s = top >> right;
+              if (kTableBits<T, V> < 16) {
+                s -= before;
+                s = s < none ? s : none;
+              }
+              const Entry c = table[s];
+#pragma unroll
+              for (int v = 0; v < V; ++v) wf[V * e + v] = c.v[v];
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) mma16(wf, tokens(u, m, f), now[m]);
+          }
+          if (u + a.parts < units) words(tile, u + a.parts, w);
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[m][i] = __builtin_fmaf(sc[i], now[m][i], acc[m][i]);
+        }
+    }
+    // sums[wave][row of 16][token]
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sums[wave * 256 + (4 * g + i) * 16 + row] = acc[m][i];
+      __syncthreads();
+      const int tokens = Q == 2 ? a.M : (a.M - 16 * m < 16 ? a.M - 16 * m : 16);
+      for (int o = tid; o < a.rows_at_once * kRowsOf * 16; o += threads) {
+        const int q = o / (kRowsOf * 16), rr = o / 16 % kRowsOf, tok = o % 16;
+        const int r = (t0 + q) * kRowsOf + rr;
+        if (tok >= tokens || t0 + q >= a.tiles || r >= a.N) continue;
+        float z = 0.f;
+        for (int p = 0; p < a.parts; ++p) {
+          const float* s = sums + (q * a.parts + p) * 256;
+          z += s[rr * 16 + tok];
+          if (Q == 2) z += s[(rr + 8) * 16 + tok + 8];
+        }
+        if (bias) z += (float)bias[r];
+        z = act_value(z, a.act);
+        const int64_t m0 = 16 * m + tok;
+        if (res) z += (float)res[m0 * a.ldr + r];
+        y[m0 * a.ldy + r] = (T)z;
+      }
+    }
+  }
+}
+
+}  // namespace qlin
+}  // namespace bcjr

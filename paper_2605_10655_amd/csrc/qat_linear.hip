@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "bcjr.h"
+#include "qat_codes_kernels.h"
 #include "qat_gemm_launch.h"
 #include "qat_linear_kernels.h"
 
@@ -21,6 +22,10 @@ QAT_GEMM_EXTERN(bf16)
 QAT_GEMM_EXTERN(f16)
 QAT_GEMM_EXTERN(float)
 #undef QAT_GEMM_EXTERN
+
+// qat_codes.hip
+bool codes_take(int k, int V, int64_t block, int64_t M, int64_t N, int64_t K);
+int codes_linear(const CodesArgs& a, int dtype, int k, int V, hipStream_t stream);
 
 namespace {
 
@@ -278,7 +283,8 @@ size_t trellis_linear_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K
   if (!dtype_ok(dtype) || !dims_ok(M, N, K) || !dims_fit(M, N, K) || !code_of(state_bits, k, V, block, &c) ||
       K % block)
     return 0;
-  return align_up((size_t)(N * K) * elem_size(dtype)) + (M ? gemm_plan(dtype, M, N, K).part : 0);
+  if (M == 0 || codes_take(c.k, c.V, c.block, M, N, K)) return 0;
+  return align_up((size_t)(N * K) * elem_size(dtype)) + gemm_plan(dtype, M, N, K).part;
 }
 
 int trellis_linear(const void* x, int64_t ldx, const uint32_t* packed, const float* codebook, int state_bits, int k,
@@ -295,9 +301,14 @@ int trellis_linear(const void* x, int64_t ldx, const uint32_t* packed, const flo
   if (!x || !packed || !codebook || !y || misaligned(x, es) || misaligned(packed, 4) || misaligned(codebook, 16) ||
       misaligned(scales, 4) || misaligned(bias, es) || misaligned(residual, es) || misaligned(y, es))
     return BCJR_ERR_INVALID_ARG;
-  if (!workspace || misaligned(workspace, 16) ||
-      ws_bytes < trellis_linear_workspace_bytes(dtype, M, N, K, state_bits, k, V, block))
-    return BCJR_ERR_WORKSPACE;
+  const size_t need = trellis_linear_workspace_bytes(dtype, M, N, K, state_bits, k, V, block);
+  if (need && (!workspace || misaligned(workspace, 16) || ws_bytes < need)) return BCJR_ERR_WORKSPACE;
+  if (codes_take(c.k, c.V, c.block, M, N, K)) {
+    const CodesArgs a = {x,      ldx, packed,     codebook, scales, bias,   residual, ldr,           y,
+                         ldy,    activation,      c.n,      (int)M, (int)N, (int)K,   (int)c.block, (int)c.words,
+                         0,      0,   0};
+    return codes_linear(a, dtype, c.k, c.V, stream);
+  }
   return by_type(dtype, [&](auto t) -> int {
     using T = decltype(t);
     T* W = static_cast<T*>(workspace);
