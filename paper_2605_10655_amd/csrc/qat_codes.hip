@@ -49,7 +49,48 @@ int by_code(const CodesArgs& a, int k, int V, hipStream_t stream) {
   return by_tokens<T, 4, 1>(a, stream);
 }
 
+template <class T, int KB, int V>
+int launch_dense(const uint32_t* packed, int64_t B, const float* codebook, int n, int64_t block, int64_t words,
+                 const float* scales, T* W, hipStream_t stream) {
+  const int64_t groups = B * (block / 8), each = (int64_t)kDenseThreads * kDenseGroups;
+  const int64_t grid = (groups + each - 1) / each;
+  const void* kernel = reinterpret_cast<const void*>(&dense_large_kernel<T, KB, V>);
+  const size_t lds = codes_table<float, V>(n);
+  if (lds > 65536 &&
+      hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+    return BCJR_ERR_HIP;
+  hipLaunchKernelGGL((dense_large_kernel<T, KB, V>), dim3((unsigned)(grid < 256 ? grid : 256)), dim3(kDenseThreads), lds,
+                     stream, packed, codebook, scales, groups, n, (int)(block / 8), (int)words, W);
+  return hipGetLastError() == hipSuccess ? BCJR_OK : BCJR_ERR_HIP;
+}
+
+template <class T>
+int dense_by_code(const uint32_t* packed, int64_t B, const float* codebook, int n, int k, int V, int64_t block,
+                  int64_t words, const float* scales, T* W, hipStream_t stream) {
+  if (V == 2) return launch_dense<T, 4, 2>(packed, B, codebook, n, block, words, scales, W, stream);
+  if (k == 1) return launch_dense<T, 1, 1>(packed, B, codebook, n, block, words, scales, W, stream);
+  if (k == 2) return launch_dense<T, 2, 1>(packed, B, codebook, n, block, words, scales, W, stream);
+  if (k == 3) return launch_dense<T, 3, 1>(packed, B, codebook, n, block, words, scales, W, stream);
+  return launch_dense<T, 4, 1>(packed, B, codebook, n, block, words, scales, W, stream);
+}
+
 }  // namespace
+
+// Whether dense_large_kernel takes a decode: codes of whole groups of eight
+// weights, and enough of them that filling the table pays.
+bool dense_large_takes(int k, int V, int64_t block, int64_t B) {
+  return ((V == 1 && k <= 4) || (V == 2 && k == 4)) && block % 8 == 0 && B * block >= ((int64_t)1 << 20) &&
+         B * (block / 8) < ((int64_t)1 << 31);
+}
+
+int dense_large(const uint32_t* packed, int64_t B, const float* codebook, int n, int k, int V, int64_t block,
+                int64_t words, const float* scales, void* W, int dtype, hipStream_t stream) {
+  if (dtype == kBF16)
+    return dense_by_code(packed, B, codebook, n, k, V, block, words, scales, static_cast<bf16*>(W), stream);
+  if (dtype == kF16)
+    return dense_by_code(packed, B, codebook, n, k, V, block, words, scales, static_cast<f16*>(W), stream);
+  return dense_by_code(packed, B, codebook, n, k, V, block, words, scales, static_cast<float*>(W), stream);
+}
 
 // Whether the kernels take a product: the trellises with 1 to 4 bits a step
 // (two weights a step with 4) and blocks of whole 256 weights (below them

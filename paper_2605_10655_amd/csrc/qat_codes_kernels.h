@@ -249,5 +249,86 @@ __global__ __launch_bounds__(64 * kCodesWaves) void codes_kernel(CodesArgs a) {
   }
 }
 
+// W = scale * codebook[state] of many weights, the product in fp32, rounded to
+// T.  A thread takes eight weights (16 bytes of a 16-bit type) in each of eight
+// rows of 8192, kept in registers while the fp32 codebook passes through LDS in
+// pieces of 128 KB; of each, states of the others read a zero.  (Read from L2
+// a weight costs 1.1 cycles a CU and requests 64 bytes for 4: 16.8 million
+// weights took 74 us.)
+constexpr int kDenseThreads = 1024, kDenseGroups = 8;
+
+template <class T, int KB, int V>
+__global__ __launch_bounds__(kDenseThreads) void dense_large_kernel(const uint32_t* __restrict__ packed,
+                                                                    const float* __restrict__ codebook,
+                                                                    const float* __restrict__ scales, int64_t groups,
+                                                                    int n, int per, int words, T* __restrict__ W) {
+  struct Entry {
+    float v[V];
+  };
+  typedef T T8 __attribute__((ext_vector_type(8)));
+  extern __shared__ __align__(16) char lds[];
+  const Entry* table = reinterpret_cast<const Entry*>(lds);
+  const int tid = threadIdx.x;
+  const int pieces = n > kTableBits<float, V> ? 1 << (n - kTableBits<float, V>) : 1;
+  const int right = 32 - n;
+  const uint32_t none = 1u << kTableBits<float, V>;
+  constexpr int kSteps = 8 / V;
+  bool filled = false;
+  for (int64_t g0 = (int64_t)blockIdx.x * kDenseThreads * kDenseGroups; g0 < groups;
+       g0 += (int64_t)gridDim.x * kDenseThreads * kDenseGroups) {
+    // a group's window begins at a multiple of 8 bits and spans at most 44
+    uint32_t hi[kDenseGroups], lo[kDenseGroups];
+    float v[kDenseGroups][8];
+#pragma unroll
+    for (int i = 0; i < kDenseGroups; ++i) {
+      int64_t g = g0 + i * kDenseThreads + tid;
+      g = g < groups ? g : groups - 1;
+      const uint32_t path = (uint32_t)g / (uint32_t)per;
+      const int at = (int)((uint32_t)g - path * per) * kSteps * KB, j = at >> 5, o = at & 31;
+      const uint32_t* p = packed + (int64_t)path * words;
+      const uint64_t w = (((uint64_t)p[j] << 32) | p[j + 1 < words ? j + 1 : j]) << o;
+      hi[i] = (uint32_t)(w >> 32);
+      lo[i] = (uint32_t)w;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+    }
+#pragma unroll 1
+    for (int h = 0; h < pieces; ++h) {
+      if (!filled || pieces > 1) {
+        __syncthreads();
+        fill_table<float, V>(reinterpret_cast<float*>(lds), codebook, n, h, tid, kDenseThreads);
+        __syncthreads();
+        filled = true;
+      }
+      const uint32_t before = (uint32_t)h << kTableBits<float, V>;
+#pragma unroll
+      for (int i = 0; i < kDenseGroups; ++i) {
+        // the states are worked out anew for each piece, not kept for all
+        asm volatile("" : "+v"(hi[i]), "+v"(lo[i]));
+#pragma unroll
+        for (int e = 0; e < kSteps; ++e) {
+          const uint32_t top = e == 0 ? hi[i] : __builtin_amdgcn_alignbit(hi[i], lo[i], 32 - KB * e);
+          uint32_t s = (top >> right) - before;
+          s = s < none ? s : none;
+          const Entry c = table[s];
+          // one piece adds the codeword, the others 0
+#pragma unroll
+          for (int u = 0; u < V; ++u) v[i][V * e + u] += c.v[u];
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kDenseGroups; ++i) {
+      const int64_t g = g0 + i * kDenseThreads + tid;
+      if (g >= groups) continue;
+      const float f = scales ? scales[(uint32_t)g / (uint32_t)per] : 1.f;
+      T8 o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = (T)scaled(f, v[i][e]);
+      __builtin_memcpy(W + g * 8, &o, sizeof(o));
+    }
+  }
+}
+
 }  // namespace qlin
 }  // namespace bcjr

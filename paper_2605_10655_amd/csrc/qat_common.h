@@ -159,5 +159,13 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   return 1.f;
 }
 
+// scale * codeword in fp32: kept from being fused with a conversion to fp16,
+// so that every type rounds the same product
+__device__ __forceinline__ float scaled(float scale, float c) {
+  float p = scale * c;
+  asm("" : "+v"(p));
+  return p;
+}
+
 }  // namespace qlin
 }  // namespace bcjr

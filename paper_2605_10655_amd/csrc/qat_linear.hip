@@ -26,6 +26,9 @@ QAT_GEMM_EXTERN(float)
 // qat_codes.hip
 bool codes_take(int k, int V, int64_t block, int64_t M, int64_t N, int64_t K);
 int codes_linear(const CodesArgs& a, int dtype, int k, int V, hipStream_t stream);
+bool dense_large_takes(int k, int V, int64_t block, int64_t B);
+int dense_large(const uint32_t* packed, int64_t B, const float* codebook, int n, int k, int V, int64_t block,
+                int64_t words, const float* scales, void* W, int dtype, hipStream_t stream);
 
 namespace {
 
@@ -91,12 +94,16 @@ bool code_of(int state_bits, int k, int V, int64_t block, Code* c) {
   return true;
 }
 
-template <class T>
-int run_dense(const uint32_t* packed, const float* codebook, const float* scales, const Code& c, int64_t B, T* W,
-              hipStream_t stream) {
-  hipLaunchKernelGGL(dense_kernel<T>, dim3((unsigned)ceil_div(B * c.steps, 256)), dim3(256), 0, stream, packed,
-                     codebook, scales, B, c.steps, c.n, c.k, c.V, c.words, W);
-  return launched();
+int run_dense(const uint32_t* packed, const float* codebook, const float* scales, const Code& c, int64_t B, void* W,
+              int dtype, hipStream_t stream) {
+  if (dense_large_takes(c.k, c.V, c.block, B))
+    return dense_large(packed, B, codebook, c.n, c.k, c.V, c.block, c.words, scales, W, dtype, stream);
+  return by_type(dtype, [&](auto t) -> int {
+    using T = decltype(t);
+    hipLaunchKernelGGL(dense_kernel<T>, dim3((unsigned)ceil_div(B * c.steps, 256)), dim3(256), 0, stream, packed,
+                       codebook, scales, B, c.steps, c.n, c.k, c.V, c.words, static_cast<T*>(W));
+    return launched();
+  });
 }
 
 // blocks of 256 threads that one launch can have
@@ -272,9 +279,7 @@ int trellis_dense(const uint32_t* packed, int64_t B, const float* codebook, int 
       misaligned(scales, 4) || misaligned(W, elem_size(dtype)))
     return BCJR_ERR_INVALID_ARG;
   if (B == 0) return BCJR_OK;
-  return by_type(dtype, [&](auto t) -> int {
-    return run_dense(packed, codebook, scales, c, B, static_cast<decltype(t)*>(W), stream);
-  });
+  return run_dense(packed, codebook, scales, c, B, W, dtype, stream);
 }
 
 size_t trellis_linear_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K, int state_bits, int k, int V,
@@ -312,7 +317,7 @@ int trellis_linear(const void* x, int64_t ldx, const uint32_t* packed, const flo
   return by_type(dtype, [&](auto t) -> int {
     using T = decltype(t);
     T* W = static_cast<T*>(workspace);
-    const int st = run_dense(packed, codebook, scales, c, N * (K / block), W, stream);
+    const int st = run_dense(packed, codebook, scales, c, N * (K / block), W, dtype, stream);
     if (st != BCJR_OK) return st;
     const GemmArgs g = {x, W, ldx, K, nullptr, M, N, K, bias, residual, ldr, y, ldy, nullptr, nullptr, activation};
     return gemm<T, kRow, kRow>(g, reinterpret_cast<char*>(W) + align_up((size_t)(N * K) * es), stream);

@@ -296,14 +296,6 @@ __global__ void unpack_kernel(const uint32_t* __restrict__ packed, int64_t B, in
   states[i] = (int32_t)window(p[j], j + 1 < words ? p[j + 1] : 0u, (int)(at & 31), n);
 }
 
-// scale * codeword in fp32: kept from being fused with a conversion to fp16,
-// so that every type rounds the same product
-__device__ __forceinline__ float scaled(float scale, float c) {
-  float p = scale * c;
-  asm("" : "+v"(p));
-  return p;
-}
-
 // W = scale * codebook[state] in fp32, rounded to T.  One thread per step.
 template <class T>
 __global__ void dense_kernel(const uint32_t* __restrict__ packed, const float* __restrict__ codebook,

@@ -356,6 +356,23 @@ def test_pack_unpack_dense(n, k, V, block, B):
         assert torch.equal(got, (s[:, None] * want).to(dt))
 
 
+@pytest.mark.parametrize("n,k,V,block,B", [(16, 2, 1, 256, 5000), (16, 4, 2, 256, 4100), (14, 3, 1, 512, 2051),
+                                           (16, 1, 1, 64, 16500), (15, 2, 1, 8, 131079), (12, 4, 1, 1000, 1051),
+                                           (6, 2, 1, 40, 30011), (16, 2, 1, 100, 11001)])
+def test_dense_of_many_weights(n, k, V, block, B):
+    """Above a million weights, where the codebook passes through LDS."""
+    _say(f"[dense many] n={n} k={k} V={V} block={block} B={B}")
+    st = R.legal_states(np.random.default_rng(n), B, block // V, n, k)
+    packed = Q.trellis_pack(torch.from_numpy(st).cuda(), n, k)
+    cb, cd = rand(n, *((1 << n,) if V == 1 else (1 << n, V)))
+    s, sc = rand(5, B)
+    want = cb[torch.from_numpy(st).long()].view(B, block)
+    assert torch.equal(Q.trellis_dense(packed, cd, n, k, V, block).cpu(), want)
+    for dt in R.TYPES.values():
+        got = Q.trellis_dense(packed, cd, n, k, V, block, scales=sc, dtype=dt).cpu()
+        assert torch.equal(got, (s[:, None] * want).to(dt))
+
+
 def test_pack_refuses_what_is_no_path():
     st = torch.from_numpy(R.legal_states(np.random.default_rng(0), 5, 20, 8, 2)).cuda()
     Q.trellis_pack(st, 8, 2)
