@@ -496,10 +496,11 @@ __device__ __forceinline__ void finish(const GemmArgs& g, int part, f32x16 (&acc
   }
 }
 
-// BT x BT of C per workgroup of four waves, W x W of them per wave in 32 x 32
-// matrix instructions, 128 bytes of k a step through two LDS buffers: while one
-// step is multiplied the next one's tiles travel, and the other workgroups of
-// the CU fill this one's waits.  COPY: both operands straight into LDS (codes
+// The smallest products, and those whose operands cannot be copied: BT x BT of
+// C per workgroup of four waves, W x W of them per wave in 32 x 32 matrix
+// instructions, 128 bytes of k a step through two LDS buffers: while one step
+// is multiplied the next one's tiles travel, and the other workgroups of the CU
+// fill this one's waits.  COPY: both operands straight into LDS (codes
 // always through registers, where they become T).
 template <class T, int AM, int BM, int BT, int W, bool COPY>
 __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
@@ -793,6 +794,148 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
   V* const in = wave < 3 ? b0 : wave < 6 ? b1 : wave == 6 ? up0 : up1;
   finish<T, 4, NJ>(g, p.part, acc, reinterpret_cast<float*>(in) + (wave < 6 ? wave % 3 : 0) * kStrip, lane, i0 + wi,
                    j0 + wj);
+}
+
+// For products of too few such tiles to fill the CUs: 128 x 128 of C per
+// workgroup of eight waves in turns, 64 x 32 of them per wave, A always copied.
+// A tile this size takes 64 bytes of copies a cycle at the matrix
+// instructions' full rate, which is all that a CU can fetch; four buffers keep
+// three steps of copies under way.
+template <class T, int AM, int BM>
+__global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int tj) {
+  constexpr int kThreads = 512, BT = 128, NI = 2;
+  using TA = Tile<T, AM, BT, kThreads>;
+  using TB = Tile<T, BM, BT, kThreads>;
+  using V = typename Vec<T>::type;
+  constexpr bool kCopyB = BM != kCodes;
+  constexpr int kBuf = TA::kChunks + TB::kChunks, kStrip = 32 * (32 + 4);
+  static_assert(2 * kStrip * 4 <= kBuf * 16, "strips fit the buffers");
+  __shared__ __align__(16) V lds0[kBuf];
+  __shared__ __align__(16) V lds1[kBuf];
+  __shared__ __align__(16) V lds2[kBuf];
+  __shared__ __align__(16) V lds3[kBuf];
+
+  const Place p = place_of(ti, tj, g.splits);
+  const int64_t i0 = (int64_t)p.i * BT, j0 = (int64_t)p.j * BT;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wi = (wave >> 2) * 64, wj = (wave & 3) * 32;
+  const bool behind = wave >= 4;
+  f32x16 acc[NI][1];
+#pragma unroll
+  for (int x = 0; x < NI; ++x)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[x][0][r] = 0.f;
+
+  // Whole steps; what is left of k goes first, on its own.
+  const int64_t all = g.K / TA::kStep;
+  const int64_t first = all * p.part / g.splits;
+  const int steps = (int)(all * (p.part + 1) / g.splits - first);
+  V fa[4][NI], fb[4];
+  auto read = [&](const V* lds) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+#pragma unroll
+      for (int x = 0; x < NI; ++x) fa[kk][x] = TA::operand(lds, wi + 32 * x, kk, lane);
+      fb[kk] = TB::operand(lds + TA::kChunks, wj, kk, lane);
+    }
+  };
+  auto multiply = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int x = 0; x < NI; ++x) mma<T>(fa[kk][x], fb[kk], acc[x][0]);
+    __builtin_amdgcn_s_setprio(0);
+  };
+  typename TB::Regs rb[2];
+  if (g.K % TA::kStep && p.part == g.splits - 1) {
+    const int64_t k0 = all * TA::kStep;
+    TA::copy_rest(g.a, g.lda, g.I, g.K, i0, k0, lds0, tid);
+    if constexpr (kCopyB) {
+      TB::copy_rest(g.b, g.ldb, g.J, g.K, j0, k0, lds0 + TA::kChunks, tid);
+    } else {
+      TB::fetch(g.b, g.ldb, g.bscales, g.J, g.K, j0, k0, rb[0], tid);
+      TB::put(rb[0], lds0 + TA::kChunks, tid);
+    }
+    wait_copies<0>();
+    lds_barrier();
+    read(lds0);
+    multiply();
+    lds_barrier();
+  }
+  if (steps > 0) {
+    typename TA::Copy ca;
+    typename TB::Copy cb;
+    typename TB::Codes codes;
+    TA::start(ca, g.a, g.lda, g.I, i0, first * TA::kStep, tid);
+    if constexpr (kCopyB)
+      TB::start(cb, g.b, g.ldb, g.J, j0, first * TA::kStep, tid);
+    else
+      TB::start_codes(codes, g.b, g.bscales, g.J, j0, first * TA::kStep, tid);
+    // step s; past the last that one again, as above
+    auto copy = [&](int s, V* lds) __attribute__((always_inline)) {
+      TA::copy(ca, lds, tid);
+      ca.base += s + 1 < steps ? ca.step : 0;
+      if constexpr (kCopyB) {
+        TB::copy(cb, lds + TA::kChunks, tid);
+        cb.base += s + 1 < steps ? cb.step : 0;
+      }
+    };
+    // codes: two steps' under way
+    auto fetch = [&](int s, int slot) __attribute__((always_inline)) {
+      if constexpr (!kCopyB) {
+        asm volatile("" ::: "memory");
+        TB::fetch_all(codes, rb[slot]);
+        asm volatile("" ::: "memory");
+        codes.base += s + 1 < steps ? codes.step * kRows : 0;
+        codes.sbase += s + 1 < steps ? codes.step * 2 : 0;
+      }
+    };
+    auto put = [&](int slot, V* lds) __attribute__((always_inline)) {
+      if constexpr (!kCopyB) TB::put(rb[slot], lds + TA::kChunks, tid);
+    };
+    constexpr int kD = TA::kPer + (kCopyB ? TB::kPer : 0), kF = kCopyB ? 0 : TB::kLoads;
+    // Step s from `now`; `last` (read by every wave in step s - 1) receives step
+    // s + 3's copies, `then` (in step s - 2) step s + 2's codes.  Two steps'
+    // copies and codes may be under way when the next step's have landed.
+    auto step = [&](int s, int slot, V* now, V* then, V* last) __attribute__((always_inline)) {
+      read(now);
+      copy(s + 3, last);
+      put(slot, then);
+      fetch(s + 4, slot);
+      wait_copies<2 * kD + 2 * kF>();
+      lds_barrier();
+      multiply();
+      lds_barrier();
+    };
+    fetch(0, 0);
+    fetch(1, 1);
+    put(0, lds0);
+    put(1, lds1);
+    copy(0, lds0);
+    copy(1, lds1);
+    copy(2, lds2);
+    fetch(2, 0);
+    fetch(3, 1);
+    wait_copies<2 * kD + 2 * kF>();
+    lds_barrier();
+    if (behind) lds_barrier();
+#pragma unroll 1
+    for (int s = 0; s < steps; s += 4) {
+      step(s, 0, lds0, lds2, lds3);
+      if (s + 1 == steps) break;
+      step(s + 1, 1, lds1, lds3, lds0);
+      if (s + 2 == steps) break;
+      step(s + 2, 0, lds2, lds0, lds1);
+      if (s + 3 == steps) break;
+      step(s + 3, 1, lds3, lds1, lds2);
+    }
+    if (!behind) lds_barrier();
+    wait_copies<0>();
+  }
+  __syncthreads();
+  V* const in = wave < 2 ? lds0 : wave < 4 ? lds1 : wave < 6 ? lds2 : lds3;
+  finish<T, NI, 1>(g, p.part, acc, reinterpret_cast<float*>(in) + (wave & 1) * kStrip, lane, i0 + wi, j0 + wj);
 }
 
 // The epilogue of a product whose k was split: the parts' sum (always in the

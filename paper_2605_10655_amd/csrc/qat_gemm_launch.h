@@ -79,7 +79,8 @@ int gemm(GemmArgs g, void* ws, hipStream_t stream) {
       hipLaunchKernelGGL((gemm_large_kernel<T, AM, BM>), dim3((unsigned)(p.ti * p.tj * p.splits)), dim3(512), 0, stream,
                          g, p.ti, p.tj);
     else if (p.tile == 128)
-      launch_gemm<T, AM, BM, 128, true>(g, p, stream);
+      hipLaunchKernelGGL((gemm_mid_kernel<T, AM, BM>), dim3((unsigned)(p.ti * p.tj * p.splits)), dim3(512), 0, stream, g,
+                         p.ti, p.tj);
     else
       launch_gemm<T, AM, BM, 64, true>(g, p, stream);
   } else {
