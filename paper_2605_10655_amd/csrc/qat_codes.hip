@@ -11,16 +11,8 @@ namespace {
 
 template <class T, int KB, int V, int MT, int Q>
 int launch(CodesArgs a, hipStream_t stream) {
-  constexpr int kRowsOf = 16 / Q;
-  const int units = (a.K / kChunk + Q - 1) / Q;
-  a.tiles = (a.N + kRowsOf - 1) / kRowsOf;
-  a.parts = 1;
-  while (a.parts < kCodesWaves && a.parts < units) a.parts *= 2;
-  // as many tiles at once as leave a workgroup for each CU
-  a.rows_at_once = kCodesWaves / a.parts;
-  while (a.rows_at_once > 1 && (a.tiles + a.rows_at_once - 1) / a.rows_at_once < 256) a.rows_at_once /= 2;
-  const int groups = (a.tiles + a.rows_at_once - 1) / a.rows_at_once;
-  const int waves = a.parts * a.rows_at_once;
+  const int groups = lay_out(a, Q, (a.K / kChunk + Q - 1) / Q);
+  const int waves = a.parts * a.at_once;
   const size_t lds = codes_table<T, V>(a.n) + (size_t)waves * 256 * sizeof(float);
   const void* kernel = reinterpret_cast<const void*>(&codes_kernel<T, KB, V, MT, Q>);
   if (lds > 65536 &&
@@ -95,9 +87,9 @@ int dense_large(const uint32_t* packed, int64_t B, const float* codebook, int n,
 // Whether the kernels take a product: the trellises with 1 to 4 bits a step
 // (two weights a step with 4) and blocks of whole 256 weights (below them
 // scales would change inside a matrix instruction).  Past 64 tokens the weights
-// are better decoded once.
+// are better decoded once, into a dense matrix.
 bool codes_take(int k, int V, int64_t block, int64_t M, int64_t N, int64_t K) {
-  return ((V == 1 && k <= 4) || (V == 2 && k == 4)) && block % kChunk == 0 && M <= 64 && N < ((int64_t)1 << 24) &&
+  return ((V == 1 && k <= 4) || (V == 2 && k == 4)) && block % kChunk == 0 && M <= kFewTokens && N < ((int64_t)1 << 24) &&
          K < ((int64_t)1 << 24);
 }
 

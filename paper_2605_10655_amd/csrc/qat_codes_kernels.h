@@ -1,26 +1,16 @@
 // qat_codes_kernels.h -- a few tokens through trellis-coded weights: the bit
 // strings are turned into operands of the matrix instructions as they are read.
 #pragma once
-#include "qat_common.h"
+#include "qat_few_kernels.h"
 
 namespace bcjr {
 namespace qlin {
 
-struct CodesArgs {
-  const void* x;
-  int64_t ldx;
+struct CodesArgs : FewArgs {
   const uint32_t* packed;
   const float* codebook;
   const float* scales;       // [N, K / block] or null
-  const void* bias;
-  const void* residual;
-  int64_t ldr;
-  void* y;
-  int64_t ldy;
-  int act, n;
-  int M, N, K, block, words;
-  int tiles;                 // tiles of rows
-  int parts, rows_at_once;   // waves along K and along tiles
+  int n, block, words;
 };
 
 // y = act(x W^T + bias) + residual for up to 16 MT tokens.
@@ -41,34 +31,7 @@ struct CodesArgs {
 // are not used, and half the rows a tile fill twice the CUs.
 //
 // Waves of a workgroup split K; their sums meet in LDS in a fixed order.
-template <class T>
-struct Frag;   // eight weights or activations of a lane
-template <>
-struct Frag<bf16> {
-  typedef bf16 type __attribute__((ext_vector_type(8)));
-};
-template <>
-struct Frag<f16> {
-  typedef f16 type __attribute__((ext_vector_type(8)));
-};
-template <>
-struct Frag<float> {
-  typedef float type __attribute__((ext_vector_type(8)));
-};
-
-__device__ __forceinline__ void mma16(const Frag<bf16>::type& a, const Frag<bf16>::type& b, f32x4& c) {
-  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ void mma16(const Frag<f16>::type& a, const Frag<f16>::type& b, f32x4& c) {
-  c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ void mma16(const Frag<float>::type& a, const Frag<float>::type& b, f32x4& c) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
-}
-
 constexpr int kChunk = 256;       // weights of a row that a wave takes at once
-constexpr int kCodesWaves = 16;
 
 
 // State bits of a part of the codebook: 128 KB
@@ -106,7 +69,7 @@ __device__ __forceinline__ void fill_table(T* table, const float* codebook, int 
 }
 
 template <class T, int KB, int V, int MT, int Q>
-__global__ __launch_bounds__(64 * kCodesWaves) void codes_kernel(CodesArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves) void codes_kernel(CodesArgs a) {
   using F = typename Frag<T>::type;
   struct Entry {
     T v[V];
@@ -124,9 +87,6 @@ __global__ __launch_bounds__(64 * kCodesWaves) void codes_kernel(CodesArgs a) {
   const int pieces = a.n > kTableBits<T, V> ? 1 << (a.n - kTableBits<T, V>) : 1;
   const int right = 32 - a.n;
   const T* x = static_cast<const T*>(a.x);
-  const T* bias = static_cast<const T*>(a.bias);
-  const T* res = static_cast<const T*>(a.residual);
-  T* y = static_cast<T*>(a.y);
 
   // the words of this lane's 64 weights of its row in unit u
   auto words = [&](int tile, int u, uint32_t* w) __attribute__((always_inline)) {
@@ -168,7 +128,7 @@ __global__ __launch_bounds__(64 * kCodesWaves) void codes_kernel(CodesArgs a) {
   };
 
   bool filled = false;
-  for (int t0 = blockIdx.x * a.rows_at_once; t0 < a.tiles; t0 += gridDim.x * a.rows_at_once) {
+  for (int t0 = blockIdx.x * a.at_once; t0 < a.tiles; t0 += gridDim.x * a.at_once) {
     const int tile = t0 + of;
     const bool live = tile < a.tiles;
     f32x4 acc[MT];
@@ -221,31 +181,8 @@ __global__ __launch_bounds__(64 * kCodesWaves) void codes_kernel(CodesArgs a) {
             for (int i = 0; i < 4; ++i) acc[m][i] = __builtin_fmaf(sc[i], now[m][i], acc[m][i]);
         }
     }
-    // sums[wave][row of 16][token]
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sums[wave * 256 + (4 * g + i) * 16 + row] = acc[m][i];
-      __syncthreads();
-      const int tokens = Q == 2 ? a.M : (a.M - 16 * m < 16 ? a.M - 16 * m : 16);
-      for (int o = tid; o < a.rows_at_once * kRowsOf * 16; o += threads) {
-        const int q = o / (kRowsOf * 16), rr = o / 16 % kRowsOf, tok = o % 16;
-        const int r = (t0 + q) * kRowsOf + rr;
-        if (tok >= tokens || t0 + q >= a.tiles || r >= a.N) continue;
-        float z = 0.f;
-        for (int p = 0; p < a.parts; ++p) {
-          const float* s = sums + (q * a.parts + p) * 256;
-          z += s[rr * 16 + tok];
-          if (Q == 2) z += s[(rr + 8) * 16 + tok + 8];
-        }
-        if (bias) z += (float)bias[r];
-        z = act_value(z, a.act);
-        const int64_t m0 = 16 * m + tok;
-        if (res) z += (float)res[m0 * a.ldr + r];
-        y[m0 * a.ldy + r] = (T)z;
-      }
-    }
+    for (int m = 0; m < MT; ++m) finish_few<T, Q>(a, sums, acc[m], t0, m, tid, threads);
   }
 }
 

@@ -61,6 +61,29 @@ int run_linear(const GemmArgs& g, int dtype, void* ws, hipStream_t stream) {
   return by_type(dtype, [&](auto t) -> int { return gemm<decltype(t), kRow, kRow>(g, ws, stream); });
 }
 
+FewArgs few_args(const void* x, int64_t ldx, const void* bias, const void* residual, int64_t ldr, void* y,
+                 int64_t ldy, int act, int64_t M, int64_t N, int64_t K) {
+  return {x, ldx, bias, residual, ldr, y, ldy, act, (int)M, (int)N, (int)K, 0, 0, 0};
+}
+
+template <class T, int MT, int Q>
+int launch_few(FewArgs a, const void* W, int64_t ldw, hipStream_t stream) {
+  const int groups = lay_out(a, Q, (a.K + 256 * Q - 1) / (256 * Q));
+  hipLaunchKernelGGL((few_kernel<T, MT, Q>), dim3((unsigned)groups), dim3((unsigned)(64 * a.parts * a.at_once)), 0,
+                     stream, a, static_cast<const T*>(W), ldw);
+  return launched();
+}
+
+// Up to 64 tokens without a checkpoint.
+int run_few(const FewArgs& a, const void* W, int64_t ldw, int dtype, hipStream_t stream) {
+  return by_type(dtype, [&](auto t) -> int {
+    using T = decltype(t);
+    if (a.M <= 8) return launch_few<T, 1, 2>(a, W, ldw, stream);
+    if (a.M <= 16) return launch_few<T, 1, 1>(a, W, ldw, stream);
+    return launch_few<T, 4, 1>(a, W, ldw, stream);
+  });
+}
+
 struct VjpPlan {
   size_t dz, part, sums, total;
 };
@@ -167,6 +190,8 @@ int qat_linear_act(const void* x, int64_t ldx, const void* W, int64_t ldw, const
     return BCJR_ERR_INVALID_ARG;
   const size_t need = qat_linear_act_workspace_bytes(dtype, M, N, K);
   if (need && (!workspace || misaligned(workspace, 16) || ws_bytes < need)) return BCJR_ERR_WORKSPACE;
+  if (M <= kFewTokens && !z_codes)
+    return run_few(few_args(x, ldx, bias, residual, ldr, y, ldy, activation, M, N, K), W, ldw, dtype, stream);
   const GemmArgs g = {x, W, ldx, ldw, nullptr, M, N, K, bias, residual, ldr, y, ldy, z_codes, z_scales, activation};
   return run_linear(g, dtype, workspace, stream);
 }
@@ -309,9 +334,14 @@ int trellis_linear(const void* x, int64_t ldx, const uint32_t* packed, const flo
   const size_t need = trellis_linear_workspace_bytes(dtype, M, N, K, state_bits, k, V, block);
   if (need && (!workspace || misaligned(workspace, 16) || ws_bytes < need)) return BCJR_ERR_WORKSPACE;
   if (codes_take(c.k, c.V, c.block, M, N, K)) {
-    const CodesArgs a = {x,      ldx, packed,     codebook, scales, bias,   residual, ldr,           y,
-                         ldy,    activation,      c.n,      (int)M, (int)N, (int)K,   (int)c.block, (int)c.words,
-                         0,      0,   0};
+    CodesArgs a = {};
+    static_cast<FewArgs&>(a) = few_args(x, ldx, bias, residual, ldr, y, ldy, activation, M, N, K);
+    a.packed = packed;
+    a.codebook = codebook;
+    a.scales = scales;
+    a.n = c.n;
+    a.block = (int)c.block;
+    a.words = (int)c.words;
     return codes_linear(a, dtype, c.k, c.V, stream);
   }
   return by_type(dtype, [&](auto t) -> int {

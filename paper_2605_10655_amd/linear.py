@@ -27,13 +27,15 @@ captured into a graph own theirs.  The autograd node is
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import dataclasses
+import functools
 import math
 
 import torch
 
-from . import _check_ws, _keep_alive, _ptr, _raise, _stream, load_library
+from . import _check_ws, _keep_alive, _raise, load_library
 
 __all__ = ["ACTIVATIONS", "Act8", "act8_store", "act8_load", "linear_act", "linear_act_vjp",
            "trellis_words", "trellis_pack", "trellis_unpack", "trellis_dense", "trellis_linear"]
@@ -77,6 +79,10 @@ def _activation(name):
     return ACTIVATIONS[name]
 
 
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 def _tensor(name, t, dtype=None, device=None):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
@@ -93,20 +99,25 @@ def _matrix(name, t, dtype=None, device=None, rows=None, cols=None):
     """(t as [rows, cols], its row stride): columns contiguous, rows not
     overlapping; more dimensions only if contiguous."""
     _tensor(name, t, dtype, device)
-    if t.dim() < 2:
-        raise ValueError(f"{name} must have at least two dimensions, got {tuple(t.shape)}")
-    if t.dim() > 2:
+    shape = t.shape
+    if len(shape) != 2:
+        if len(shape) < 2:
+            raise ValueError(f"{name} must have at least two dimensions, got {tuple(shape)}")
         if not t.is_contiguous():
             raise ValueError(f"{name} with more than two dimensions must be contiguous")
-        t = t.view(math.prod(t.shape[:-1]), t.shape[-1])
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        t = t.view(math.prod(shape[:-1]), shape[-1])
+        shape = t.shape
+    n, c = shape
+    if (rows is not None and n != rows) or (cols is not None and c != cols):
         raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, "
-                         f"{'cols' if cols is None else cols}], got {tuple(t.shape)}")
-    ld = t.shape[1] if t.shape[0] <= 1 else t.stride(0)
-    if (t.shape[1] > 1 and t.stride(1) != 1) or ld < t.shape[1]:
+                         f"{'cols' if cols is None else cols}], got {tuple(shape)}")
+    ld, one = t.stride()
+    if n <= 1:
+        ld = c
+    if (c > 1 and one != 1) or ld < c:
         raise ValueError(f"{name} must have contiguous columns and rows that do not overlap, "
                          f"got strides {t.stride()}")
-    return t, max(int(ld), 1)
+    return t, max(ld, 1)
 
 
 def _vector(name, t, n, dtype, device):
@@ -149,17 +160,44 @@ def _space(workspace, nbytes, device):
     if workspace is not None:
         _check_ws(workspace, device)
         return workspace
-    return torch.empty(int(nbytes), dtype=torch.uint8, device=device) if nbytes else None
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
 def _size(ws):
     return 0 if ws is None else ws.numel() * ws.element_size()
 
 
+# Workspace sizes are arithmetic on the arguments: asked for once each.
+@functools.lru_cache(maxsize=4096)
+def _linear_bytes(*args):
+    return int(_lib().qat_linear_act_workspace_bytes(*args))
+
+
+@functools.lru_cache(maxsize=4096)
+def _vjp_bytes(*args):
+    return int(_lib().qat_linear_act_vjp_workspace_bytes(*args))
+
+
+@functools.lru_cache(maxsize=4096)
+def _trellis_bytes(*args):
+    return int(_lib().trellis_linear_workspace_bytes(*args))
+
+
+_HERE = contextlib.nullcontext()
+
+
 def _on(stream, device):
+    """The tensors' device as the current one for a call's launches."""
     if stream is not None and stream.device != device:
         raise ValueError(f"stream is on {stream.device}, the call's tensors on {device}")
-    return torch.cuda.device(device)
+    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _stream(stream, device):
+    """The stream's handle: the device's current stream unless one is given."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 # ---------------------------------------------------------------- 8-bit checkpoints
@@ -215,7 +253,7 @@ def act8_store(x, *, stream=None) -> Act8:
     with _on(stream, dev):
         a = _new_act8(m.shape[0], m.shape[1], m.dtype, dev)
         rc = lib.qat_act8_store(_ptr(m), DTYPES[m.dtype], m.shape[0], m.shape[1], ld, _ptr(a.codes),
-                                _ptr(a.scales), _stream(stream))
+                                _ptr(a.scales), _stream(stream, dev))
         _raise("qat_act8_store", rc)
         _keep_alive(stream, a.codes, a.scales)
     return a
@@ -233,7 +271,7 @@ def act8_load(a: Act8, dtype=None, *, out=None, stream=None):
     with _on(stream, dev):
         out = _output("out", out, (a.rows, a.cols), dtype, dev, a.codes, a.scales)
         rc = lib.qat_act8_load(_ptr(a.codes), _ptr(a.scales), a.rows, a.cols, _ptr(out), DTYPES[dtype],
-                               a.cols, _stream(stream))
+                               a.cols, _stream(stream, dev))
         _raise("qat_act8_load", rc)
         _keep_alive(stream, out)
     return out
@@ -259,10 +297,10 @@ def linear_act(x, W, bias=None, residual=None, activation="none", *, out=None, s
     with _on(stream, dev):
         y = _output("out", out, (*x.shape[:-1], N), t, dev, m, w, bias, res)
         z8 = _new_act8(M, N, torch.float32, dev) if save else None
-        ws = _space(workspace, lib.qat_linear_act_workspace_bytes(DTYPES[t], M, N, K), dev)
+        ws = _space(workspace, _linear_bytes(DTYPES[t], M, N, K), dev)
         rc = lib.qat_linear_act(_ptr(m), ldx, _ptr(w), ldw, _ptr(bias), _ptr(res), ldr, DTYPES[t], act, M,
                                 N, K, _ptr(y), N, _ptr(z8.codes) if save else None,
-                                _ptr(z8.scales) if save else None, _ptr(ws), _size(ws), _stream(stream))
+                                _ptr(z8.scales) if save else None, _ptr(ws), _size(ws), _stream(stream, dev))
         _raise("qat_linear_act", rc)
         _keep_alive(stream, y, ws, *((z8.codes, z8.scales) if save else ()))
     return (y, z8) if save else y
@@ -298,18 +336,19 @@ def linear_act_vjp(dy, x8, W, z8=None, activation="none", *, want_dx=True, want_
         dx = torch.empty((*dy.shape[:-1], K), dtype=t, device=dev) if want_dx else None
         dW = torch.empty((N, K), dtype=t, device=dev) if want_dW else None
         db = torch.empty(N, dtype=t, device=dev) if want_dbias else None
-        ws = _space(workspace, lib.qat_linear_act_vjp_workspace_bytes(DTYPES[t], M, N, K, act), dev)
+        ws = _space(workspace, _vjp_bytes(DTYPES[t], M, N, K, act), dev)
         rc = lib.qat_linear_act_vjp(_ptr(d), ldd, _ptr(x8.codes) if want_dW else None,
                                     _ptr(x8.scales) if want_dW else None, _ptr(w), ldw,
                                     _ptr(z8.codes) if act else None, _ptr(z8.scales) if act else None,
                                     DTYPES[t], act, M, N, K, _ptr(dx), _ptr(dW), _ptr(db), _ptr(ws),
-                                    _size(ws), _stream(stream))
+                                    _size(ws), _stream(stream, dev))
         _raise("qat_linear_act_vjp", rc)
         _keep_alive(stream, dx, dW, db, ws)
     return dx, dW, db
 
 
 # ---------------------------------------------------------------- trellis codes
+@functools.lru_cache(maxsize=1024)
 def _code(state_bits, k, V, block):
     words = int(_lib().trellis_words(int(state_bits), int(k), int(V), int(block)))
     if words == 0:
@@ -340,7 +379,7 @@ def trellis_pack(states, state_bits: int, k: int, *, check=True, stream=None):
         packed = torch.empty((*states.shape[:-1], words), dtype=torch.int32, device=dev)
         bad = torch.empty(1, dtype=torch.int32, device=dev) if check else None
         rc = lib.trellis_pack(_ptr(states), B, steps, int(state_bits), int(k), _ptr(packed), _ptr(bad),
-                              _stream(stream))
+                              _stream(stream, dev))
         _raise("trellis_pack", rc)
         _keep_alive(stream, packed, bad)
         if check:
@@ -362,7 +401,7 @@ def trellis_unpack(packed, state_bits: int, k: int, steps: int, *, stream=None):
     with _on(stream, dev):
         states = torch.empty((*packed.shape[:-1], steps), dtype=torch.int32, device=dev)
         rc = lib.trellis_unpack(_ptr(packed), math.prod(packed.shape[:-1]), steps, int(state_bits), int(k),
-                                _ptr(states), _stream(stream))
+                                _ptr(states), _stream(stream, dev))
         _raise("trellis_unpack", rc)
         _keep_alive(stream, states)
     return states
@@ -400,7 +439,7 @@ def trellis_dense(packed, codebook, state_bits: int, k: int, V: int = 1, block: 
     with _on(stream, dev):
         W = torch.empty((B, block), dtype=dtype, device=dev)
         rc = lib.trellis_dense(_ptr(packed), B, _ptr(codebook), int(state_bits), int(k), int(V), int(block),
-                               _ptr(scales), _ptr(W), DTYPES[dtype], _stream(stream))
+                               _ptr(scales), _ptr(W), DTYPES[dtype], _stream(stream, dev))
         _raise("trellis_dense", rc)
         _keep_alive(stream, W)
     return W
@@ -426,11 +465,11 @@ def trellis_linear(x, packed, codebook, state_bits: int, k: int, V: int = 1, blo
     res, ldr = (None, 0) if residual is None else _matrix("residual", residual, t, dev, M, N)
     with _on(stream, dev):
         y = _output("out", out, (*x.shape[:-1], N), t, dev, m, packed, codebook, scales, bias, res)
-        ws = _space(workspace, lib.trellis_linear_workspace_bytes(DTYPES[t], M, N, K, int(state_bits),
-                                                                  int(k), int(V), int(block)), dev)
+        ws = _space(workspace, _trellis_bytes(DTYPES[t], M, N, K, int(state_bits), int(k), int(V),
+                                              int(block)), dev)
         rc = lib.trellis_linear(_ptr(m), ldx, _ptr(packed), _ptr(codebook), int(state_bits), int(k), int(V),
                                 int(block), _ptr(scales), _ptr(bias), _ptr(res), ldr, DTYPES[t], act, M, N, K,
-                                _ptr(y), N, _ptr(ws), _size(ws), _stream(stream))
+                                _ptr(y), N, _ptr(ws), _size(ws), _stream(stream, dev))
         _raise("trellis_linear", rc)
         _keep_alive(stream, y, ws)
     return y

@@ -114,7 +114,11 @@ def _check_linear(host, devi, act, dt, what):
     y, yb, z, zb = R.linear64(*host, act, dt)
     got, z8 = Q.linear_act(*devi, act, save=True)
     within(got, y, yb, what)
-    assert torch.equal(Q.linear_act(*devi, act), got)   # without the checkpoint the same
+    # without the checkpoint: up to 64 tokens by another kernel, which adds the
+    # K products in another order; the bound holds for any order
+    plain = Q.linear_act(*devi, act)
+    within(plain, y, yb, what + " without checkpoint")
+    assert len(y) <= 64 or torch.equal(plain, got)
     # the checkpoint: half a step off, the step not larger than need be
     v = R.values64(z8.codes.cpu(), z8.scales.cpu(), z.shape[0])
     M, N = z.shape
@@ -178,14 +182,16 @@ def test_non_finite_values_stay_in_their_rows(t):
     dt = R.TYPES[t]
     for M in (6, 90):
         host, devi = _layer(M, M, 72, 64, dt)
-        y = Q.linear_act(*devi, "silu")
-        _, z8 = Q.linear_act(*devi, "silu", save=True)
+        y, z8 = Q.linear_act(*devi, "silu", save=True)
+        plain = Q.linear_act(*devi, "silu")
         bad = [2, M - 1]
         devi[0][2] = float("nan")
         devi[0][M - 1] = float("inf")
         got, g8 = Q.linear_act(*devi, "silu", save=True)
         keep = [i for i in range(M) if i not in bad]
         assert torch.equal(got[keep], y[keep]) and not torch.isfinite(got[2]).any()
+        got = Q.linear_act(*devi, "silu")
+        assert torch.equal(got[keep], plain[keep]) and not torch.isfinite(got[2]).any()
         v = R.values64(g8.codes.cpu(), g8.scales.cpu(), M)
         assert torch.isfinite(v[keep]).all() and torch.isnan(v[2]).all()
         assert (g8.scales[0] < 0).all()
