@@ -279,7 +279,8 @@ int qat_sgd_step(float *param, const float *grad, int64_t count, float lr, float
  * fp32.  Matrices are row-major with a leading dimension in elements (ldx >=
  * columns); pointers are aligned to their element, codes to 16 bytes.  Inputs
  * and outputs must not overlap.  Rows up to 2^31 - 1, columns up to 2^22 - 1,
- * else BCJR_ERR_UNSUPPORTED.  Every call gives the same bits each time. */
+ * leading dimensions of x, W and dy below 32 MiB, else BCJR_ERR_UNSUPPORTED.
+ * Every call gives the same bits each time. */
 #define QAT_F32 0
 #define QAT_BF16 1
 #define QAT_F16 2

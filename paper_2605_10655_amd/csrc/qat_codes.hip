@@ -89,7 +89,7 @@ int dense_large(const uint32_t* packed, int64_t B, const float* codebook, int n,
 // scales would change inside a matrix instruction).  Past 64 tokens the weights
 // are better decoded once, into a dense matrix.
 bool codes_take(int k, int V, int64_t block, int64_t M, int64_t N, int64_t K) {
-  return ((V == 1 && k <= 4) || (V == 2 && k == 4)) && block % kChunk == 0 && M <= kFewTokens && N < ((int64_t)1 << 24) &&
+  return ((V == 1 && k <= 4) || (V == 2 && k == 4)) && block % kChunk == 0 && M <= 64 && N < ((int64_t)1 << 24) &&
          K < ((int64_t)1 << 24);
 }
 

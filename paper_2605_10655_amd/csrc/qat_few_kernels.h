@@ -33,7 +33,6 @@ __device__ __forceinline__ void mma16(const Frag<float>::type& a, const Frag<flo
 }
 
 constexpr int kFewWaves = 16;     // of a workgroup at most
-constexpr int kFewTokens = 64;
 
 // What both kernels of few tokens share: the layer's operands but the weights,
 // and how a workgroup's waves are laid over it.
@@ -115,7 +114,7 @@ __device__ __forceinline__ typename Frag<T>::type eight(const T* p, int n) {
   return v;
 }
 
-// y = act(x W^T + bias) + residual for up to 16 MT tokens: bound by reading W.
+// y = act(x W^T + bias) + residual for up to 16 tokens: bound by reading W.
 //
 // A wave takes 16 / Q rows and 256 Q weights of each, all loads of which are
 // under way at once (8 KB of 16-bit weights).  Lane l of a matrix instruction
@@ -124,7 +123,7 @@ __device__ __forceinline__ typename Frag<T>::type eight(const T* p, int n) {
 // 8..15 are the same rows 64 bytes on, so that a load takes whole 128-byte
 // lines; tokens 8..15 are then the same tokens there, the products of unlike
 // halves are not used, and half the rows a tile fill twice the CUs.
-template <class T, int MT, int Q>
+template <class T, int Q>
 __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewArgs a, const T* W, int64_t ldw) {
   using F = typename Frag<T>::type;
   constexpr int kRowsOf = 16 / Q, kUnit = 256 * Q;
@@ -134,48 +133,37 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewArgs a, const T*
   const int row = lane & 15, g = lane >> 4;
   const int t0 = blockIdx.x * a.at_once, tile = t0 + of;
   const T* x = static_cast<const T*>(a.x);
-  f32x4 acc[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   if (tile < a.tiles) {
     int r = tile * kRowsOf + row % kRowsOf;
     r = r < a.N ? r : a.N - 1;
     // of this lane's row, and of its token
     const int k0 = (row / kRowsOf) * 32 + 8 * g, kx = (Q == 2 ? row >> 3 : 0) * 32 + 8 * g;
     const T* wr = W + r * ldw;
-    const T* xr[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      int tok = Q == 2 ? lane & 7 : 16 * m + row;
-      tok = tok < a.M ? tok : a.M - 1;
-      xr[m] = x + tok * a.ldx;
-    }
+    int tok = Q == 2 ? lane & 7 : row;
+    tok = tok < a.M ? tok : a.M - 1;
+    const T* xr = x + tok * a.ldx;
     for (int u = part * kUnit; u < a.K; u += a.parts * kUnit) {
       F w[8];
       if (u + kUnit <= a.K) {
 #pragma unroll
         for (int f = 0; f < 8; ++f) __builtin_memcpy(&w[f], wr + u + 32 * Q * f + k0, sizeof(F));
 #pragma unroll
-        for (int f = 0; f < 8; ++f)
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            F v;
-            __builtin_memcpy(&v, xr[m] + u + 32 * Q * f + kx, sizeof(F));
-            mma16(w[f], v, acc[m]);
-          }
+        for (int f = 0; f < 8; ++f) {
+          F v;
+          __builtin_memcpy(&v, xr + u + 32 * Q * f + kx, sizeof(F));
+          mma16(w[f], v, acc);
+        }
       } else {
 #pragma unroll 1
         for (int f = 0; f < 8; ++f) {
           const int k = u + 32 * Q * f;
-          const F wf = eight<T>(wr + k + k0, a.K - k - k0);
-#pragma unroll
-          for (int m = 0; m < MT; ++m) mma16(wf, eight<T>(xr[m] + k + kx, a.K - k - kx), acc[m]);
+          mma16(eight<T>(wr + k + k0, a.K - k - k0), eight<T>(xr + k + kx, a.K - k - kx), acc);
         }
       }
     }
   }
-#pragma unroll
-  for (int m = 0; m < MT; ++m) finish_few<T, Q>(a, sums, acc[m], t0, m, tid, blockDim.x);
+  finish_few<T, Q>(a, sums, acc, t0, 0, tid, blockDim.x);
 }
 
 }  // namespace qlin

@@ -106,6 +106,7 @@ struct Tile {
     int64_t step;
   };
 
+  template <bool TO_LDS = true>
   static __device__ __forceinline__ void start(Copy& s, const void* p, int64_t ld, int64_t rows, int64_t r0,
                                                int64_t k0, int tid) {
     const uint32_t ldb = (uint32_t)(ld * (int64_t)sizeof(T));
@@ -114,13 +115,14 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int at = i * THREADS + tid;
-      const int line = at / kLine, c = (at % kLine) ^ swizzle(line);
+      // (through registers the places are swizzled on the way to LDS)
+      const int line = at / kLine, c = TO_LDS ? (at % kLine) ^ swizzle(line) : at % kLine;
       if (MODE == kRow) {
         const int r = row_of(line);
         s.off[i] = (uint32_t)(r < last ? r : last - 1) * ldb + c * 16;
       } else {
         const int r = row_of(c * E);
-        s.off[i] = (uint32_t)line * ldb + (r < last ? r : last - E) * (int)sizeof(T);
+        s.off[i] = (uint32_t)line * ldb + (r < last ? r : (TO_LDS ? last - E : 0)) * (int)sizeof(T);
       }
     }
     const int64_t first = MODE == kRow ? r0 * ld + k0 : k0 * ld + r0;
@@ -243,6 +245,17 @@ struct Tile {
       __builtin_memcpy(&g.v[i], &v, 16);
       g.s[i] = __builtin_amdgcn_raw_buffer_load_b16(s, (int)c.soff[i], 0, 0);
     }
+  }
+
+  // The same of whole steps: every chunk by one load.  (A column chunk that runs
+  // past the last row reads on into what follows it in memory, which the k
+  // after the last whole step leave room for: slack(); those sums are not
+  // stored.)
+  static __device__ __forceinline__ int64_t slack(int64_t ld) { return MODE == kCol ? (E + ld - 1) / ld : 0; }
+
+  static __device__ __forceinline__ void fetch_whole(const Copy& s, Regs& g) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) __builtin_memcpy(&g.v[i], s.base + s.off[i], 16);
   }
 
   static __device__ __forceinline__ void put(const Regs& g, V* lds, int tid) {
@@ -497,27 +510,29 @@ __device__ __forceinline__ void finish(const GemmArgs& g, int part, f32x16 (&acc
 }
 
 // The smallest products, and those whose operands cannot be copied: BT x BT of
-// C per workgroup of four waves, W x W of them per wave in 32 x 32 matrix
-// instructions, 128 bytes of k a step through two LDS buffers: while one step
-// is multiplied the next one's tiles travel, and the other workgroups of the CU
-// fill this one's waits.  COPY: both operands straight into LDS (codes
-// always through registers, where they become T).
-template <class T, int AM, int BM, int BT, int W, bool COPY>
+// C per workgroup of four waves, a quarter each in 32 x 32 matrix instructions,
+// 128 bytes of k a step through four LDS buffers.  COPY: both operands straight
+// into LDS, three steps under way; otherwise through registers, four steps
+// under way (codes always so, becoming T on the way).  No step has a branch:
+// what is left of k beyond whole steps goes first, and steps past the last
+// fetch that one again, into buffers that nothing reads any more.
+template <class T, int AM, int BM, int BT, bool COPY>
 __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
-  constexpr int kThreads = 256, NT = W / 32;
-  static_assert((BT / W) * (BT / W) == 4, "four waves");
+  constexpr int kThreads = 256, W = BT / 2, NT = W / 32;
   using TA = Tile<T, AM, BT, kThreads>;
   using TB = Tile<T, BM, BT, kThreads>;
   using V = typename Vec<T>::type;
   constexpr bool kCopyA = COPY && AM != kCodes, kCopyB = COPY && BM != kCodes;
-  // Two buffers of their own names: the compiler then knows that a copy into
-  // one does not touch what is read from the other, and waits for neither.  The
+  // Buffers of their own names: the compiler then knows that a copy into one
+  // does not touch what is read from another, and waits for neither.  The
   // epilogue's strips (32 rows x W sums a wave, rows padded by 16 bytes) lie in
-  // them, half of the waves in each.
+  // them, a wave's in each.
   constexpr int kBuf = TA::kChunks + TB::kChunks, kStrip = 32 * (W + 4);
-  static_assert(2 * kStrip * 4 <= kBuf * 16, "strips fit the buffers");
+  static_assert(kStrip * 4 <= kBuf * 16, "a strip fits a buffer");
   __shared__ __align__(16) V lds0[kBuf];
   __shared__ __align__(16) V lds1[kBuf];
+  __shared__ __align__(16) V lds2[kBuf];
+  __shared__ __align__(16) V lds3[kBuf];
 
   const Place p = place_of(ti, tj, g.splits);
   const int64_t i0 = (int64_t)p.i * BT, j0 = (int64_t)p.j * BT;
@@ -531,56 +546,12 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
 
-  const int64_t all = (g.K + TA::kStep - 1) / TA::kStep;
+  // Whole steps; through registers a few k stay after them.
+  const int64_t sa = COPY ? 0 : TA::slack(g.lda), sb = COPY ? 0 : TB::slack(g.ldb), after = sa > sb ? sa : sb;
+  const int64_t all = g.K > after ? (g.K - after) / TA::kStep : 0;
   const int64_t first = all * p.part / g.splits;
   const int steps = (int)(all * (p.part + 1) / g.splits - first);
-  typename TA::Regs ra;
-  typename TB::Regs rb;
-  typename TA::Copy ca;
-  typename TB::Copy cb;
-  if constexpr (kCopyA) TA::start(ca, g.a, g.lda, g.I, i0, first * TA::kStep, tid);
-  if constexpr (kCopyB) TB::start(cb, g.b, g.ldb, g.J, j0, first * TA::kStep, tid);
-  auto copy = [&](int s, V* lds) __attribute__((always_inline)) {
-    if (s >= steps) return;
-    const int64_t k0 = (first + s) * TA::kStep;
-    if (k0 + TA::kStep <= g.K) {
-      if constexpr (kCopyA) {
-        TA::copy(ca, lds, tid);
-        ca.base += ca.step;
-      }
-      if constexpr (kCopyB) {
-        TB::copy(cb, lds + TA::kChunks, tid);
-        cb.base += cb.step;
-      }
-    } else {
-      if constexpr (kCopyA) TA::copy_rest(g.a, g.lda, g.I, g.K, i0, k0, lds, tid);
-      if constexpr (kCopyB) TB::copy_rest(g.b, g.ldb, g.J, g.K, j0, k0, lds + TA::kChunks, tid);
-    }
-  };
-  // operands through registers: one step's under way.  (The fences keep these
-  // loads younger than the copies before them.)
-  auto fetch = [&](int s) __attribute__((always_inline)) {
-    asm volatile("" ::: "memory");
-    if (s >= steps) return;
-    const int64_t k0 = (first + s) * TA::kStep;
-    if constexpr (!kCopyA) TA::fetch(g.a, g.lda, nullptr, g.I, g.K, i0, k0, ra, tid);
-    if constexpr (!kCopyB) TB::fetch(g.b, g.ldb, g.bscales, g.J, g.K, j0, k0, rb, tid);
-    asm volatile("" ::: "memory");
-  };
-  auto put = [&](int s, V* lds) __attribute__((always_inline)) {
-    if (s >= steps) return;
-    if constexpr (!kCopyA) TA::put(ra, lds, tid);
-    if constexpr (!kCopyB) TB::put(rb, lds + TA::kChunks, tid);
-  };
-  auto step = [&](int s, V* now, V* other) __attribute__((always_inline)) {
-    // This step's tiles have landed (the codes of the next, loaded after its
-    // copies, may be under way), and no wave still reads the other buffer.
-    if (kCopyA && !kCopyB && s + 1 < steps)
-      wait_copies<TB::kLoads>();
-    else if (kCopyA || kCopyB)
-      wait_copies<0>();
-    lds_barrier();
-    copy(s + 1, other);
+  auto products = [&](const V* now) __attribute__((always_inline)) {
     V fa[4][NT], fb[4][NT];
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk)
@@ -595,22 +566,110 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
       for (int x = 0; x < NT; ++x)
 #pragma unroll
         for (int y = 0; y < NT; ++y) mma<T>(fa[kk][x], fb[kk][y], acc[x][y]);
-    put(s + 1, other);
-    fetch(s + 2);
   };
+  // (one step's worth, or through registers up to two)
+  if (p.part == g.splits - 1)
+#pragma unroll 1
+    for (int64_t k0 = all * TA::kStep; k0 < g.K; k0 += TA::kStep) {
+      typename TA::Regs ra;
+      typename TB::Regs rb;
+      if constexpr (kCopyA) {
+        TA::copy_rest(g.a, g.lda, g.I, g.K, i0, k0, lds0, tid);
+      } else {
+        TA::fetch(g.a, g.lda, nullptr, g.I, g.K, i0, k0, ra, tid);
+        TA::put(ra, lds0, tid);
+      }
+      if constexpr (kCopyB) {
+        TB::copy_rest(g.b, g.ldb, g.J, g.K, j0, k0, lds0 + TA::kChunks, tid);
+      } else {
+        TB::fetch(g.b, g.ldb, g.bscales, g.J, g.K, j0, k0, rb, tid);
+        TB::put(rb, lds0 + TA::kChunks, tid);
+      }
+      wait_copies<0>();
+      lds_barrier();
+      products(lds0);
+      lds_barrier();
+    }
   if (steps > 0) {
-    fetch(0);
-    copy(0, lds0);
+    typename TA::Copy ca;
+    typename TB::Copy cb;
+    typename TB::Codes codes;
+    // slots of registers for the operands that take them
+    typename TA::Regs ra[4];
+    typename TB::Regs rb[4];
+    TA::template start<kCopyA>(ca, g.a, g.lda, g.I, i0, first * TA::kStep, tid);
+    if constexpr (BM == kCodes)
+      TB::start_codes(codes, g.b, g.bscales, g.J, j0, first * TA::kStep, tid);
+    else
+      TB::template start<kCopyB>(cb, g.b, g.ldb, g.J, j0, first * TA::kStep, tid);
+    auto copy = [&](int s, V* lds) __attribute__((always_inline)) {
+      if constexpr (kCopyA) {
+        TA::copy(ca, lds, tid);
+        ca.base += s + 1 < steps ? ca.step : 0;
+      }
+      if constexpr (kCopyB) {
+        TB::copy(cb, lds + TA::kChunks, tid);
+        cb.base += s + 1 < steps ? cb.step : 0;
+      }
+    };
+    auto fetch = [&](int s, int slot) __attribute__((always_inline)) {
+      asm volatile("" ::: "memory");
+      if constexpr (!kCopyA) {
+        TA::fetch_whole(ca, ra[slot]);
+        ca.base += s + 1 < steps ? ca.step : 0;
+      }
+      if constexpr (BM == kCodes) {
+        TB::fetch_all(codes, rb[slot]);
+        codes.base += s + 1 < steps ? codes.step * kRows : 0;
+        codes.sbase += s + 1 < steps ? codes.step * 2 : 0;
+      } else if constexpr (!kCopyB) {
+        TB::fetch_whole(cb, rb[slot]);
+        cb.base += s + 1 < steps ? cb.step : 0;
+      }
+      asm volatile("" ::: "memory");
+    };
+    auto put = [&](int slot, V* lds) __attribute__((always_inline)) {
+      if constexpr (!kCopyA) TA::put(ra[slot], lds, tid);
+      if constexpr (!kCopyB) TB::put(rb[slot], lds + TA::kChunks, tid);
+    };
+    // Two steps' copies, and the codes loaded after them, may be under way when
+    // a step's copies have landed.
+    constexpr int kD = (kCopyA ? TA::kPer : 0) + (kCopyB ? TB::kPer : 0);
+    constexpr int kF = kCopyA && !kCopyB ? TB::kLoads : 0;
+    // Step s from `now`; `last` (read by every wave in step s - 1) receives step
+    // s + 3's copies, `then` (in step s - 2) step s + 2's registers.
+    auto step = [&](int s, int slot, V* now, V* then, V* last) __attribute__((always_inline)) {
+      if (kD > 0) wait_copies<2 * kD + 2 * kF>();
+      lds_barrier();
+      copy(s + 3, last);
+      put(slot, then);
+      fetch(s + 6, slot);
+      products(now);
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) fetch(i, i);
     put(0, lds0);
-    fetch(1);
-  }
-  for (int s = 0; s < steps; s += 2) {
-    step(s, lds0, lds1);
-    if (s + 1 < steps) step(s + 1, lds1, lds0);
+    put(1, lds1);
+    copy(0, lds0);
+    copy(1, lds1);
+    copy(2, lds2);
+#pragma unroll
+    for (int i = 2; i < 6; ++i) fetch(i, i & 3);
+#pragma unroll 1
+    for (int s = 0; s < steps; s += 4) {
+      step(s, 2, lds0, lds2, lds3);
+      if (s + 1 == steps) break;
+      step(s + 1, 3, lds1, lds3, lds0);
+      if (s + 2 == steps) break;
+      step(s + 2, 0, lds2, lds0, lds1);
+      if (s + 3 == steps) break;
+      step(s + 3, 1, lds3, lds1, lds2);
+    }
+    wait_copies<0>();
   }
   __syncthreads();
-  finish<T, NT, NT>(g, p.part, acc, reinterpret_cast<float*>(wave < 2 ? lds0 : lds1) + (wave & 1) * kStrip, lane,
-                    i0 + wi, j0 + wj);
+  V* const in = wave == 0 ? lds0 : wave == 1 ? lds1 : wave == 2 ? lds2 : lds3;
+  finish<T, NT, NT>(g, p.part, acc, reinterpret_cast<float*>(in), lane, i0 + wi, j0 + wj);
 }
 
 // The same for large products: 256 x 256 of C per workgroup of eight waves, 128
@@ -637,7 +696,7 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
   using TB = Tile<T, BM, 256, kThreads>;
   using V = typename Vec<T>::type;
   constexpr bool kCopyB = BM != kCodes;
-  // tiles of their own names, as above
+  // tiles of their own names (see gemm_kernel)
   __shared__ __align__(16) V up0[TA::kChunks];
   __shared__ __align__(16) V up1[TA::kChunks];
   __shared__ __align__(16) V low0[TA::kChunks];
@@ -872,7 +931,7 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
       TB::start(cb, g.b, g.ldb, g.J, j0, first * TA::kStep, tid);
     else
       TB::start_codes(codes, g.b, g.bscales, g.J, j0, first * TA::kStep, tid);
-    // step s; past the last that one again, as above
+    // step s; past the last that one again (see gemm_large_kernel)
     auto copy = [&](int s, V* lds) __attribute__((always_inline)) {
       TA::copy(ca, lds, tid);
       ca.base += s + 1 < steps ? ca.step : 0;
@@ -940,48 +999,67 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
 
 // The epilogue of a product whose k was split: the parts' sum (always in the
 // same order), bias, activation, residual.  A thread per value, or with a
-// checkpoint per group of 32 rows of one column.
+// checkpoint per four rows of a group of one column, eight of which agree on
+// the group's scale through LDS.
 template <class T, bool CODES>
-__global__ void join_kernel(GemmArgs g) {
+__global__ __launch_bounds__(256) void join_kernel(GemmArgs g) {
+  constexpr int kShare = 8, kN = CODES ? kRows / kShare : 1, kWide = 256 / kShare;
+  __shared__ uint32_t tops[kShare][kWide];
+  __shared__ int bads[kShare][kWide];
+  const int lane = threadIdx.x % kWide, share = CODES ? threadIdx.x / kWide : 0;
   const T* bias = static_cast<const T*>(g.bias);
   const T* res = static_cast<const T*>(g.residual);
-  const int64_t j = (int64_t)blockIdx.y * blockDim.x + threadIdx.x, size = g.I * g.J;
-  if (j >= g.J) return;
-  const float b = bias ? (float)bias[j] : 0.f;
-  constexpr int kN = CODES ? kRows : 1;
-  const int64_t i0 = (int64_t)blockIdx.x * kN;
+  const int64_t j = CODES ? (int64_t)blockIdx.y * kWide + lane : (int64_t)blockIdx.y * 256 + threadIdx.x;
+  const int64_t size = g.I * g.J, i0 = CODES ? (int64_t)blockIdx.x * kRows + share * kN : (int64_t)blockIdx.x;
   float z[kN];
 #pragma unroll
-  for (int r = 0; r < kN; ++r) {
-    z[r] = 0.f;
-    if (i0 + r < g.I) {
-      const float* p = g.part + (i0 + r) * g.J + j;
-      float s = 0.f;
-      for (int q = 0; q < g.splits; ++q) s += p[q * size];
-      z[r] = s + b;
-    }
+  for (int r = 0; r < kN; ++r) z[r] = 0.f;
+  if (j < g.J) {
+    const float b = bias ? (float)bias[j] : 0.f;
+    const float* p[kN];
+#pragma unroll
+    for (int r = 0; r < kN; ++r) p[r] = g.part + (i0 + r < g.I ? i0 + r : g.I - 1) * g.J + j;
+#pragma unroll 8
+    for (int q = 0; q < g.splits; ++q)
+#pragma unroll
+      for (int r = 0; r < kN; ++r) z[r] += p[r][q * size];
+#pragma unroll
+    for (int r = 0; r < kN; ++r) z[r] = i0 + r < g.I ? z[r] + b : 0.f;
   }
   if (CODES) {
-    float amax = 0.f;
-    bool bad = false;
+    // the largest finite magnitude, and whether all are finite
+    uint32_t top = 0;
+    int bad = 0;
 #pragma unroll
     for (int r = 0; r < kN; ++r) {
-      if (finite_bits(z[r]))
-        amax = fmaxf(amax, fabsf(z[r]));
+      const uint32_t m = __float_as_uint(z[r]) & 0x7fffffffu;
+      if (m < 0x7f800000u)
+        top = m > top ? m : top;
       else
-        bad = true;
+        bad = 1;
     }
-    const Q8 q = q8_of(amax, kEmin<float>, kEmax<float>);
-    const int64_t at = blockIdx.x * g.J + j;
+    tops[share][lane] = top;
+    bads[share][lane] = bad;
+    __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kN; r += 4) {
-      uint32_t w = 0;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) w |= (uint32_t)(q8_code(z[(r + u) % kN], q) & 255) << (8 * u);
-      *reinterpret_cast<uint32_t*>(g.zcodes + at * kRows + r) = w;
+    for (int q = 0; q < kShare; ++q) {
+      top = tops[q][lane] > top ? tops[q][lane] : top;
+      bad |= bads[q][lane];
     }
-    g.zscales[at] = q8_scale_bits(q, bad);
+    if (j < g.J) {
+      const Q8 q = q8_of(__uint_as_float(top), kEmin<float>, kEmax<float>);
+      const int64_t at = blockIdx.x * g.J + j;
+#pragma unroll
+      for (int r = 0; r < kN; r += 4) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) w |= (uint32_t)(q8_code(z[(r + u) % kN], q) & 255) << (8 * u);
+        *reinterpret_cast<uint32_t*>(g.zcodes + at * kRows + share * kN + r) = w;
+      }
+      if (share == 0) g.zscales[at] = q8_scale_bits(q, bad != 0);
+    }
   }
+  if (j >= g.J) return;
 #pragma unroll
   for (int r = 0; r < kN; ++r) {
     const int64_t i = i0 + r;

@@ -30,30 +30,44 @@ struct GemmPlan {
   size_t part;     // bytes of the partial sums
 };
 
+// The tile and split that a model of the kernels' times finds shortest, in
+// cycles: a step of 128 bytes of k, what a workgroup takes before and after its
+// steps, and the workgroups that run at once (each measured); the parts of a
+// split are written, read and joined in a launch of their own.  A part has at
+// least four steps.
 inline GemmPlan gemm_plan(int dtype, int64_t I, int64_t J, int64_t K) {
-  GemmPlan p;
-  p.tile = 64;
-  for (int t : {256, 128})
-    if (ceil_div(I, t) * ceil_div(J, t) >= 200) {
-      p.tile = t;
-      break;
+  struct Kind {
+    int tile;
+    double step, fixed;
+    int at_once;
+  };
+  static constexpr Kind half[] = {{256, 2400, 9000, 256}, {128, 750, 4000, 256}, {64, 480, 3000, 512}};
+  static constexpr Kind full[] = {{256, 8600, 12000, 256}, {128, 2300, 5000, 256}, {64, 1150, 3500, 512}};
+  const int64_t steps = ceil_div(K, dtype == kF32 ? 32 : 64);
+  GemmPlan best = {};
+  double least = 0.;
+  for (const Kind& k : dtype == kF32 ? full : half) {
+    const int64_t ti = ceil_div(I, k.tile), tj = ceil_div(J, k.tile), tiles = ti * tj;
+    for (int64_t s = 1; s == 1 || (s <= steps / 4 && s <= 64 && tiles * s <= 2 * k.at_once); ++s) {
+      const double rounds = (double)ceil_div(tiles * s, k.at_once);
+      double t = rounds * ((double)ceil_div(steps, s) * k.step + k.fixed);
+      if (s > 1) t += 9000. + (double)(s * I * J) * 8. / 2000.;
+      if (best.tile == 0 || t < least) {
+        least = t;
+        best.tile = k.tile;
+        best.ti = (int)ti;
+        best.tj = (int)tj;
+        best.splits = (int)s;
+      }
     }
-  p.ti = (int)ceil_div(I, p.tile);
-  p.tj = (int)ceil_div(J, p.tile);
-  const int64_t steps = ceil_div(K, dtype == kF32 ? 32 : 64), tiles = (int64_t)p.ti * p.tj;
-  p.splits = 1;
-  if (tiles < 200) {
-    const int64_t by_fill = 256 / tiles, by_length = steps / 8;
-    p.splits = (int)(by_fill < by_length ? by_fill : by_length);
-    if (p.splits < 1) p.splits = 1;
   }
-  p.part = p.splits > 1 ? align_up((size_t)p.splits * I * J * sizeof(float)) : 0;
-  return p;
+  best.part = best.splits > 1 ? align_up((size_t)best.splits * I * J * sizeof(float)) : 0;
+  return best;
 }
 
 template <class T, int AM, int BM, int BT, bool COPY>
 void launch_gemm(const GemmArgs& g, const GemmPlan& p, hipStream_t stream) {
-  hipLaunchKernelGGL((gemm_kernel<T, AM, BM, BT, BT / 2, COPY>), dim3((unsigned)(p.ti * p.tj * p.splits)), dim3(256),
+  hipLaunchKernelGGL((gemm_kernel<T, AM, BM, BT, COPY>), dim3((unsigned)(p.ti * p.tj * p.splits)), dim3(256),
                      0, stream, g, p.ti, p.tj);
 }
 
@@ -84,7 +98,7 @@ int gemm(GemmArgs g, void* ws, hipStream_t stream) {
     else
       launch_gemm<T, AM, BM, 64, true>(g, p, stream);
   } else {
-    if (p.tile == 256) {   // the large kernel copies A (k is not split here)
+    if (p.tile == 256) {   // the large kernels copy A
       p.ti = (int)ceil_div(g.I, 128);
       p.tj = (int)ceil_div(g.J, 128);
     }
@@ -96,7 +110,7 @@ int gemm(GemmArgs g, void* ws, hipStream_t stream) {
   if (launched() != BCJR_OK) return BCJR_ERR_HIP;
   if (p.splits > 1) {
     if (g.zcodes)
-      hipLaunchKernelGGL((join_kernel<T, true>), group_grid(g.I, g.J, 64), dim3(64), 0, stream, g);
+      hipLaunchKernelGGL((join_kernel<T, true>), group_grid(g.I, g.J, 32), dim3(256), 0, stream, g);
     else
       hipLaunchKernelGGL((join_kernel<T, false>), dim3((unsigned)g.I, (unsigned)ceil_div(g.J, 256)), dim3(256), 0,
                          stream, g);

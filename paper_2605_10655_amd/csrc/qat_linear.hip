@@ -39,6 +39,8 @@ int elem_size(int dtype) { return dtype == kF32 ? 4 : 2; }
 bool dtype_ok(int dtype) { return dtype == kF32 || dtype == kBF16 || dtype == kF16; }
 bool act_ok(int act) { return act >= kActNone && act <= kActGeluTanh; }
 bool dims_ok(int64_t M, int64_t N, int64_t K) { return M >= 0 && N >= 1 && K >= 1; }
+// a tile's rows stay within 32-bit offsets
+bool strides_fit(int64_t a, int64_t b, size_t es) { return a * (int64_t)es < (1 << 25) && b * (int64_t)es < (1 << 25); }
 bool dims_fit(int64_t M, int64_t N, int64_t K) { return M < kMaxRows && N < kMaxCols && K < kMaxCols; }
 template <class F>
 int by_type(int dtype, F f) {
@@ -66,21 +68,21 @@ FewArgs few_args(const void* x, int64_t ldx, const void* bias, const void* resid
   return {x, ldx, bias, residual, ldr, y, ldy, act, (int)M, (int)N, (int)K, 0, 0, 0};
 }
 
-template <class T, int MT, int Q>
+template <class T, int Q>
 int launch_few(FewArgs a, const void* W, int64_t ldw, hipStream_t stream) {
   const int groups = lay_out(a, Q, (a.K + 256 * Q - 1) / (256 * Q));
-  hipLaunchKernelGGL((few_kernel<T, MT, Q>), dim3((unsigned)groups), dim3((unsigned)(64 * a.parts * a.at_once)), 0,
+  hipLaunchKernelGGL((few_kernel<T, Q>), dim3((unsigned)groups), dim3((unsigned)(64 * a.parts * a.at_once)), 0,
                      stream, a, static_cast<const T*>(W), ldw);
   return launched();
 }
 
-// Up to 64 tokens without a checkpoint.
+// Up to 16 tokens without a checkpoint.  (More are quicker in the products'
+// tiles: 32 tokens through 8192 x 8192 take 46 us there, 64 us here.)
 int run_few(const FewArgs& a, const void* W, int64_t ldw, int dtype, hipStream_t stream) {
   return by_type(dtype, [&](auto t) -> int {
     using T = decltype(t);
-    if (a.M <= 8) return launch_few<T, 1, 2>(a, W, ldw, stream);
-    if (a.M <= 16) return launch_few<T, 1, 1>(a, W, ldw, stream);
-    return launch_few<T, 4, 1>(a, W, ldw, stream);
+    if (a.M <= 8) return launch_few<T, 2>(a, W, ldw, stream);
+    return launch_few<T, 1>(a, W, ldw, stream);
   });
 }
 
@@ -182,15 +184,15 @@ int qat_linear_act(const void* x, int64_t ldx, const void* W, int64_t ldw, const
   if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || ldx < K || ldw < K || ldy < N ||
       (residual && ldr < N) || (!z_codes != !z_scales))
     return BCJR_ERR_INVALID_ARG;
-  if (!dims_fit(M, N, K)) return BCJR_ERR_UNSUPPORTED;
-  if (M == 0) return BCJR_OK;
   const size_t es = elem_size(dtype);
+  if (!dims_fit(M, N, K) || !strides_fit(ldx, ldw, es)) return BCJR_ERR_UNSUPPORTED;
+  if (M == 0) return BCJR_OK;
   if (!x || !W || !y || misaligned(x, es) || misaligned(W, es) || misaligned(y, es) || misaligned(bias, es) ||
       misaligned(residual, es) || misaligned(z_codes, 16) || misaligned(z_scales, 2))
     return BCJR_ERR_INVALID_ARG;
   const size_t need = qat_linear_act_workspace_bytes(dtype, M, N, K);
   if (need && (!workspace || misaligned(workspace, 16) || ws_bytes < need)) return BCJR_ERR_WORKSPACE;
-  if (M <= kFewTokens && !z_codes)
+  if (M <= 16 && !z_codes)
     return run_few(few_args(x, ldx, bias, residual, ldr, y, ldy, activation, M, N, K), W, ldw, dtype, stream);
   const GemmArgs g = {x, W, ldx, ldw, nullptr, M, N, K, bias, residual, ldr, y, ldy, z_codes, z_scales, activation};
   return run_linear(g, dtype, workspace, stream);
@@ -207,9 +209,9 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
                        size_t ws_bytes, hipStream_t stream) {
   if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || ldd < N || (dx && ldw < K))
     return BCJR_ERR_INVALID_ARG;
-  if (!dims_fit(M, N, K) || !bands_fit(M, N)) return BCJR_ERR_UNSUPPORTED;
-  if (!dx && !dW && !dbias) return BCJR_OK;
   const size_t es = elem_size(dtype);
+  if (!dims_fit(M, N, K) || !bands_fit(M, N) || !strides_fit(ldd, dx ? ldw : 1, es)) return BCJR_ERR_UNSUPPORTED;
+  if (!dx && !dW && !dbias) return BCJR_OK;
   if (misaligned(dy, es) || misaligned(W, es) || misaligned(dx, es) || misaligned(dW, es) || misaligned(dbias, es) ||
       misaligned(x_codes, 16) || misaligned(z_codes, 16) || misaligned(x_scales, 2) || misaligned(z_scales, 2))
     return BCJR_ERR_INVALID_ARG;
@@ -325,9 +327,9 @@ int trellis_linear(const void* x, int64_t ldx, const uint32_t* packed, const flo
   if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || !code_of(state_bits, k, V, block, &c) ||
       K % block || ldx < K || ldy < N || (residual && ldr < N))
     return BCJR_ERR_INVALID_ARG;
-  if (!dims_fit(M, N, K) || !threads_fit(N * K)) return BCJR_ERR_UNSUPPORTED;
-  if (M == 0) return BCJR_OK;
   const size_t es = elem_size(dtype);
+  if (!dims_fit(M, N, K) || !threads_fit(N * K) || !strides_fit(ldx, 1, es)) return BCJR_ERR_UNSUPPORTED;
+  if (M == 0) return BCJR_OK;
   if (!x || !packed || !codebook || !y || misaligned(x, es) || misaligned(packed, 4) || misaligned(codebook, 16) ||
       misaligned(scales, 4) || misaligned(bias, es) || misaligned(residual, es) || misaligned(y, es))
     return BCJR_ERR_INVALID_ARG;

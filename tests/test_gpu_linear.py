@@ -114,11 +114,11 @@ def _check_linear(host, devi, act, dt, what):
     y, yb, z, zb = R.linear64(*host, act, dt)
     got, z8 = Q.linear_act(*devi, act, save=True)
     within(got, y, yb, what)
-    # without the checkpoint: up to 64 tokens by another kernel, which adds the
+    # without the checkpoint: up to 16 tokens by another kernel, which adds the
     # K products in another order; the bound holds for any order
     plain = Q.linear_act(*devi, act)
     within(plain, y, yb, what + " without checkpoint")
-    assert len(y) <= 64 or torch.equal(plain, got)
+    assert len(y) <= 16 or torch.equal(plain, got)
     # the checkpoint: half a step off, the step not larger than need be
     v = R.values64(z8.codes.cpu(), z8.scales.cpu(), z.shape[0])
     M, N = z.shape
