@@ -86,10 +86,14 @@ int dense_large(const uint32_t* packed, int64_t B, const float* codebook, int n,
 
 // Whether the kernels take a product: the trellises with 1 to 4 bits a step
 // (two weights a step with 4) and blocks of whole 256 weights (below them
-// scales would change inside a matrix instruction).  Past 64 tokens the weights
-// are better decoded once, into a dense matrix.
+// scales would change inside a matrix instruction).  Past 16 tokens a lane's
+// products outlast its decoding, and weights decoded once into a dense matrix
+// do better unless they are so few that a second launch is what counts
+// (bf16, 16 state bits, 2 bits a step, us, this against decoding first:
+// 2048 x 2048 with 32 tokens 16.9 and 24.9, 2048 x 8192 with 64 57.8 and 39.8).
 bool codes_take(int k, int V, int64_t block, int64_t M, int64_t N, int64_t K) {
-  return ((V == 1 && k <= 4) || (V == 2 && k == 4)) && block % kChunk == 0 && M <= 64 && N < ((int64_t)1 << 24) &&
+  return ((V == 1 && k <= 4) || (V == 2 && k == 4)) && block % kChunk == 0 &&
+         (M <= 16 || (M <= 64 && N * K <= ((int64_t)1 << 22))) && N < ((int64_t)1 << 24) &&
          K < ((int64_t)1 << 24);
 }
 

@@ -74,12 +74,11 @@ __device__ __forceinline__ void finish_few(const FewArgs& a, float* sums, const 
   const T* res = static_cast<const T*>(a.residual);
   T* y = static_cast<T*>(a.y);
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 4; ++i) sums[wave * 256 + (4 * (lane >> 4) + i) * 16 + (lane & 15)] = acc[i];
+  *reinterpret_cast<f32x4*>(sums + wave * 256 + (lane & 15) * 16 + 4 * (lane >> 4)) = acc;
   __syncthreads();
   const int tokens = a.M - 16 * m < 16 ? a.M - 16 * m : 16;
   // neighbouring threads take neighbouring rows: a token's outputs are
-  // contiguous
+  // contiguous, and so are its sums in LDS
   for (int o = tid; o < a.at_once * kRowsOf * 16; o += threads) {
     const int row = o % (a.at_once * kRowsOf), tok = o / (a.at_once * kRowsOf);
     const int q = row / kRowsOf, rr = row % kRowsOf, r = t0 * kRowsOf + row;
@@ -87,8 +86,8 @@ __device__ __forceinline__ void finish_few(const FewArgs& a, float* sums, const 
     float z = 0.f;
     for (int p = 0; p < a.parts; ++p) {
       const float* s = sums + (q * a.parts + p) * 256;
-      z += s[rr * 16 + tok];
-      if (Q == 2) z += s[(rr + 8) * 16 + tok + 8];
+      z += s[tok * 16 + rr];
+      if (Q == 2) z += s[(tok + 8) * 16 + rr + 8];
     }
     if (bias) z += (float)bias[r];
     z = act_value(z, a.act);
@@ -127,7 +126,7 @@ template <class T, int Q>
 __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewArgs a, const T* W, int64_t ldw) {
   using F = typename Frag<T>::type;
   constexpr int kRowsOf = 16 / Q, kUnit = 256 * Q;
-  __shared__ float sums[kFewWaves * 256];
+  __shared__ __align__(16) float sums[kFewWaves * 256];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int part = wave % a.parts, of = wave / a.parts;
   const int row = lane & 15, g = lane >> 4;
