@@ -38,7 +38,7 @@ DEPENDS = SOURCES + [os.path.join(CSRC, f) for f in (
     "bcjr_device.h", "bcjr_kernels.h", "bcjr_vec_kernels.h", "bcjr_qat.h", "bcjr_internal.h",
     "bcjr_generic_kernels.h", "bcjr_ldlq_kernels.h", "bcjr_rot_kernels.h", "bcjr_pruned_kernels.h",
     "bcjr_lin_kernels.h", "qat_common.h", "qat_linear_kernels.h",
-    "qat_codes_kernels.h", "qat_few_kernels.h",
+    "qat_codes_kernels.h", "qat_few_kernels.h", "qat_small_kernels.h",
     "qat_gemm_kernels.h", "qat_gemm_launch.h")] + [
     os.path.join(INCLUDE, "bcjr.h")]
 

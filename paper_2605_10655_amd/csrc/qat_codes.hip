@@ -12,7 +12,9 @@ namespace {
 template <class T, int KB, int V, int MT, int Q>
 int launch(CodesArgs a, hipStream_t stream) {
   const int groups = lay_out(a, Q, (a.K / kChunk + Q - 1) / Q);
-  const int waves = a.parts * a.at_once;
+  // a large table is filled by 16 waves, of which those past parts * at_once do
+  // nothing else (14 state bits, 4096 x 256 weights: 5.5 us, with 4 waves 7.4)
+  const int waves = (V << a.n) > 64 * 32 * a.parts * a.at_once ? kFewWaves : a.parts * a.at_once;
   const size_t lds = codes_table<T, V>(a.n) + (size_t)waves * 256 * sizeof(float);
   const void* kernel = reinterpret_cast<const void*>(&codes_kernel<T, KB, V, MT, Q>);
   if (lds > 65536 &&

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   bool filled = false;
   for (int t0 = blockIdx.x * a.at_once; t0 < a.tiles; t0 += gridDim.x * a.at_once) {
     const int tile = t0 + of;
-    const bool live = tile < a.tiles;
+    const bool live = of < a.at_once && tile < a.tiles;
     f32x4 acc[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};

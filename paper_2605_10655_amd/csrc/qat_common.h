@@ -159,8 +159,8 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   return 1.f;
 }
 
-// scale * codeword in fp32: kept from being fused with a conversion to fp16,
-// so that every type rounds the same product
+// scale * c in fp32: kept from being fused with what follows (a conversion to
+// fp16, a sum), so that every type and kernel rounds the same product
 __device__ __forceinline__ float scaled(float scale, float c) {
   float p = scale * c;
   asm("" : "+v"(p));

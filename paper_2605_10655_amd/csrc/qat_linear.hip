@@ -10,6 +10,7 @@
 #include "qat_codes_kernels.h"
 #include "qat_gemm_launch.h"
 #include "qat_linear_kernels.h"
+#include "qat_small_kernels.h"
 
 namespace bcjr {
 namespace qlin {
@@ -86,13 +87,40 @@ int run_few(const FewArgs& a, const void* W, int64_t ldw, int dtype, hipStream_t
   });
 }
 
+// A layer this small has its backward pass in one launch (figures of both sides
+// beside the kernel).
+bool small_vjp(int64_t M, int64_t N, int64_t K) {
+  return M >= 1 && M <= 1024 && N <= 1024 && M * N * K <= ((int64_t)1 << 22);
+}
+
+int waves_along(int64_t terms) {
+  int parts = 1;
+  while (parts < kFewWaves && parts * 32 < terms) parts *= 2;
+  return parts;
+}
+
+template <class T>
+int run_small_vjp(SmallVjp a, hipStream_t stream) {
+  a.xparts = waves_along(a.N);
+  a.wparts = waves_along(a.M);
+  int waves = a.xparts > a.wparts ? a.xparts : a.wparts;
+  waves = waves < 4 ? 4 : waves;
+  const int64_t k = ceil_div(a.K, 16);
+  a.xblocks = a.dx ? (int)ceil_div(ceil_div(a.M, 16) * k, waves / a.xparts) : 0;
+  const int64_t wtiles = a.dW ? ceil_div(a.N, 16) * k : a.dbias ? ceil_div(a.N, 16) : 0;
+  hipLaunchKernelGGL(vjp_small_kernel<T>, dim3((unsigned)(a.xblocks + ceil_div(wtiles, waves / a.wparts))),
+                     dim3((unsigned)(64 * waves)), 0, stream, a);
+  return launched();
+}
+
 struct VjpPlan {
   size_t dz, part, sums, total;
 };
 
 // dz, the groups' sums of dbias, then the partial sums of the products
 VjpPlan vjp_plan(int dtype, int64_t M, int64_t N, int64_t K, int act) {
-  VjpPlan p;
+  VjpPlan p = {};
+  if (small_vjp(M, N, K)) return p;
   p.dz = act == kActNone ? 0 : align_up((size_t)(M * N) * elem_size(dtype));
   p.part = align_up((size_t)(ceil_div(M, kRows) * N) * sizeof(float));
   const size_t dx = M ? gemm_plan(dtype, M, K, N).part : 0, dW = gemm_plan(dtype, N, K, M).part;
@@ -129,6 +157,23 @@ int run_dense(const uint32_t* packed, const float* codebook, const float* scales
                        codebook, scales, B, c.steps, c.n, c.k, c.V, c.words, static_cast<T*>(W));
     return launched();
   });
+}
+
+template <class T, int MT>
+int launch_small(SmallCodes a, hipStream_t stream) {
+  const int groups = lay_out(a, 16, (a.K + kSmallUnit - 1) / kSmallUnit);
+  hipLaunchKernelGGL((codes_small_kernel<T, MT>), dim3((unsigned)groups), dim3((unsigned)(64 * a.parts * a.at_once)),
+                     0, stream, a);
+  return launched();
+}
+
+// Up to 16 tokens and so few weights that filling a table of the codebook for
+// them, or a second launch, is what would count (of 16384 columns 16 tokens take
+// 18.7 us in one launch, 11 in two; figures of others beside the kernel).
+bool small_codes(const Code& c, int64_t M, int64_t N, int64_t K) {
+  if (M > 16 || K > 8192 || N * K > ((int64_t)1 << 20)) return false;
+  const int64_t table = (int64_t)c.V << (c.n + 4), few = (int64_t)1 << 16;
+  return !codes_take(c.k, c.V, c.block, M, N, K) || N * K <= (table > few ? table : few);
 }
 
 // blocks of 256 threads that one launch can have
@@ -218,6 +263,11 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
   if (M > 0 && (!dy || (dx && !W) || (dW && (!x_codes || !x_scales)) ||
                 (activation != kActNone && (!z_codes || !z_scales))))
     return BCJR_ERR_INVALID_ARG;
+  if (small_vjp(M, N, K)) {
+    const SmallVjp a = {dy, ldd, x_codes, x_scales, W, ldw, z_codes, z_scales, activation, (int)M, (int)N, (int)K,
+                        dx, dW, dbias, 0, 0, 0};
+    return by_type(dtype, [&](auto t) -> int { return run_small_vjp<decltype(t)>(a, stream); });
+  }
   const VjpPlan p = vjp_plan(dtype, M, N, K, activation);
   if (p.total && (!workspace || misaligned(workspace, 16) || ws_bytes < p.total)) return BCJR_ERR_WORKSPACE;
   return by_type(dtype, [&](auto t) -> int {
@@ -315,7 +365,7 @@ size_t trellis_linear_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K
   if (!dtype_ok(dtype) || !dims_ok(M, N, K) || !dims_fit(M, N, K) || !code_of(state_bits, k, V, block, &c) ||
       K % block)
     return 0;
-  if (M == 0 || codes_take(c.k, c.V, c.block, M, N, K)) return 0;
+  if (M == 0 || small_codes(c, M, N, K) || codes_take(c.k, c.V, c.block, M, N, K)) return 0;
   return align_up((size_t)(N * K) * elem_size(dtype)) + gemm_plan(dtype, M, N, K).part;
 }
 
@@ -335,6 +385,22 @@ int trellis_linear(const void* x, int64_t ldx, const uint32_t* packed, const flo
     return BCJR_ERR_INVALID_ARG;
   const size_t need = trellis_linear_workspace_bytes(dtype, M, N, K, state_bits, k, V, block);
   if (need && (!workspace || misaligned(workspace, 16) || ws_bytes < need)) return BCJR_ERR_WORKSPACE;
+  if (small_codes(c, M, N, K)) {
+    SmallCodes a = {};
+    static_cast<FewArgs&>(a) = few_args(x, ldx, bias, residual, ldr, y, ldy, activation, M, N, K);
+    a.packed = packed;
+    a.codebook = codebook;
+    a.scales = scales;
+    a.n = c.n;
+    a.k = c.k;
+    a.V = c.V;
+    a.block = (int)c.block;
+    a.words = (int)c.words;
+    return by_type(dtype, [&](auto t) -> int {
+      using T = decltype(t);
+      return M == 1 ? launch_small<T, 1>(a, stream) : M <= 4 ? launch_small<T, 4>(a, stream) : launch_small<T, 16>(a, stream);
+    });
+  }
   if (codes_take(c.k, c.V, c.block, M, N, K)) {
     CodesArgs a = {};
     static_cast<FewArgs&>(a) = few_args(x, ldx, bias, residual, ldr, y, ldy, activation, M, N, K);

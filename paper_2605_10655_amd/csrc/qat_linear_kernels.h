@@ -172,7 +172,8 @@ __global__ __launch_bounds__(kGroupThreads) void act8_load_kernel(const int8_t* 
 // ---------------------------------------------------------------- backward
 // dz = dy * act'(z8), rounded to T for the matrix instructions (half a step of
 // the type each, as dy itself), and the sum of the unrounded dz over each
-// group's rows.
+// group's rows.  Small layers have dz and these sums by themselves, by the same
+// operations in the same order: dbias does not depend on what else is wanted.
 template <class T, int ACT>
 __global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__ dy, int64_t ldd,
                                                            const int8_t* __restrict__ zcodes,
@@ -184,7 +185,7 @@ __global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__
   if (b.n == 0) return;
   const int64_t at = b.g * cols + b.c;
   const int left = rows - b.g * kRows < kRows ? (int)(rows - b.g * kRows) : kRows;
-  float sum[C] = {};
+  float eights[4][C] = {};   // sums of eight rows
   u32x4 w[C][2];
   uint16_t s[C];
   if (ACT != kActNone)
@@ -206,19 +207,19 @@ __global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__
     for (int i = 0; i < 16; ++i) {
       if (ACT != kActNone) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) v[i][c] *= act_slope(q8_value(code_at(&w[c][h], i), s[c]), ACT);
+        for (int c = 0; c < C; ++c) v[i][c] = scaled(act_slope(q8_value(code_at(&w[c][h], i), s[c]), ACT), v[i][c]);
       }
       if (16 * h + i < left) {
         if (ACT != kActNone) set<T, C>(dst + i * cols, b.n, v[i]);
 #pragma unroll
-        for (int c = 0; c < C; ++c) sum[c] += v[i][c];
+        for (int c = 0; c < C; ++c) eights[2 * h + i / 8][c] += v[i][c];
       }
     }
   }
   if (part)
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      if (c < b.n) part[at + c] = sum[c];
+      if (c < b.n) part[at + c] = (eights[0][c] + eights[1][c]) + (eights[2][c] + eights[3][c]);
 }
 
 // The groups' sums of a column, in 64 bits and a fixed order: 16 threads take

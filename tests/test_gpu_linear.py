@@ -244,8 +244,20 @@ def test_vjp_large_tiles(t, I, J, K, pad):
 
 
 @pytest.mark.parametrize("t", R.TYPES)
+@pytest.mark.parametrize("M,N,K", [(1024, 17, 33), (1025, 17, 33), (7, 1024, 40), (7, 1025, 40), (1, 1, 70000),
+                                   (129, 300, 111), (64, 256, 256), (64, 256, 257), (2, 2, 3)])
+def test_vjp_at_the_bounds_of_its_small_form(t, M, N, K):
+    """One launch for up to 2^22 products and 1024 terms of a sum, several past
+    them."""
+    _say(f"[vjp bounds] {t} {M}x{N}x{K}")
+    ref, call = _vjp_case(M + 3 * N, M, N, K, R.TYPES[t], "gelu_tanh", 5, dense=True)
+    for got, r, b, what in zip(Q.linear_act_vjp(*call), ref[::2], ref[1::2], ("dx", "dW", "dbias")):
+        within(got, r, b, f"{what} {t} {M}x{N}x{K}")
+
+
+@pytest.mark.parametrize("t", R.TYPES)
 @pytest.mark.parametrize("act", R.ACTS)
-@pytest.mark.parametrize("M,pad", [(1, 0), (40, 3), (150, 8)])
+@pytest.mark.parametrize("M,pad", [(1, 0), (40, 3), (150, 8), (400, 1)])
 def test_vjp_forms(t, act, M, pad):
     _say(f"[vjp forms] {t} {act} M={M}")
     ref, call = _vjp_case(M, M, 136, 96, R.TYPES[t], act, pad)
@@ -436,6 +448,44 @@ def test_trellis_linear(t, n, k, V, block, N, nb, M):
     assert torch.equal(Q.trellis_linear(xd, packed.view(N, nb, -1), cd, n, k, V, block), got)
 
 
+@pytest.mark.parametrize("t", R.TYPES)
+@pytest.mark.parametrize("n,k,V,block,N,K", [
+    (16, 2, 1, 256, 1030, 1024), (16, 4, 2, 512, 4100, 512), (16, 4, 2, 256, 2049, 1024), (15, 1, 1, 256, 520, 1024),
+    (14, 3, 1, 256, 1025, 256), (9, 2, 1, 128, 1030, 1024), (11, 4, 1, 8448, 5, 8448), (7, 5, 3, 96, 11, 8256)])
+@pytest.mark.parametrize("M", [1, 8, 9, 40])
+def test_trellis_linear_of_many_weights(t, n, k, V, block, N, K, M):
+    """More weights or longer rows than one launch takes in fp32: a table of
+    the codebook in LDS, or a dense matrix first."""
+    dt = R.TYPES[t]
+    _say(f"[trellis many] {t} n={n} k={k} V={V} block={block} {M}x{N}x{K}")
+    W, s, packed, cd, sd = _coded(n + N, N, K, n, k, V, block)
+    x, xd = rand(M, M, K, dtype=dt, scale=K ** -0.5)
+    Ws = (s[:, :, None].double() * W.double()).reshape(N, K)
+    # the weights: one rounding to the type, and one by their scale
+    y, yb, _, _ = R.linear64(x, Ws, None, None, "silu", dt, w_err=2.1 * R.HALF[dt])
+    within(Q.trellis_linear(xd, packed, cd, n, k, V, block, scales=sd, activation="silu"), y, yb, "scaled")
+
+
+@pytest.mark.parametrize("t", R.TYPES)
+@pytest.mark.parametrize("n,k,V,block,N,nb", [(16, 2, 1, 256, 3, 32), (13, 5, 1, 7, 40, 9), (5, 1, 8, 8, 33, 65),
+                                              (16, 16, 1, 3, 9, 4), (9, 3, 2, 10, 1, 1)])
+@pytest.mark.parametrize("M", [1, 2, 4, 5, 16])
+def test_few_weights_are_multiplied_in_fp32(t, n, k, V, block, N, nb, M):
+    """No rounding of a weight to the type: the bound of fp32 sums alone."""
+    dt = R.TYPES[t]
+    K = block * nb
+    _say(f"[trellis small] {t} n={n} k={k} V={V} block={block} {M}x{N}x{K}")
+    W, s, packed, cd, sd = _coded(n + N, N, K, n, k, V, block)
+    x, xd = rand(M, M, K, dtype=dt, scale=K ** -0.5, pad=M % 3)
+    b, bd = rand(7, N, dtype=dt)
+    r, rd = rand(8, M, N, dtype=dt)
+    Ws = (s[:, :, None].double() * W.double()).reshape(N, K)
+    # the product with the scale is rounded once, to fp32
+    y, yb, _, _ = R.linear64(x, Ws, b, r, "gelu", dt, w_err=1.1 * R.HALF[torch.float32])
+    within(Q.trellis_linear(xd, packed, cd, n, k, V, block, scales=sd, bias=bd, residual=rd, activation="gelu"),
+           y, yb, "small")
+
+
 def test_trellis_linear_of_no_tokens_and_of_three_dimensions():
     W, s, packed, cd, sd = _coded(3, 12, 64, 8, 2, 1, 32)
     x = torch.randn(2, 3, 64, device="cuda")
@@ -488,6 +538,8 @@ def test_refusals():
     big = torch.zeros(8, 64, device="cuda")
     with pytest.raises(ValueError):
         Q.linear_act(big[:4], torch.zeros(64, 64, device="cuda"), out=big[3:7])
+    x = torch.zeros(17, 64, device="cuda")
+    Q.trellis_linear(x, packed, cb, **ok)
     with pytest.raises(P.BcjrError):
         Q.trellis_linear(x, packed, cb, **ok, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
 
