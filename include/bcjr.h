@@ -278,9 +278,12 @@ int qat_sgd_step(float *param, const float *grad, int64_t count, float lr, float
  * gradients and of the matrix instructions' operands; every sum is held in
  * fp32.  Matrices are row-major with a leading dimension in elements (ldx >=
  * columns); pointers are aligned to their element, codes to 16 bytes.  Inputs
- * and outputs must not overlap.  Rows up to 2^31 - 1, columns up to 2^22 - 1,
- * leading dimensions of x, W and dy below 32 MiB, else BCJR_ERR_UNSUPPORTED.
- * Every call gives the same bits each time. */
+ * and outputs must not overlap, nor the workspaces of calls that may run at
+ * the same time.  Rows up to 2^31 - 1, columns up to 2^22 - 1, leading
+ * dimensions of x, W and dy below 32 MiB, and below 2^32 threads a launch (of
+ * which one covers at least 32 values, in trellis_pack, _unpack and _dense one
+ * state), else BCJR_ERR_UNSUPPORTED.  Every call gives the same bits each
+ * time; how many tokens share a call may change an output's last bits. */
 #define QAT_F32 0
 #define QAT_BF16 1
 #define QAT_F16 2
@@ -320,7 +323,8 @@ int qat_linear_act(const void *x, int64_t ldx, const void *W, int64_t ldw, const
  * with z [M, N] and x [M, K] read from their checkpoints (z is unused for
  * QAT_ACT_NONE).  dx [M, K], dW [N, K] and dbias [N] are dense; NULL where
  * unwanted, and then W (dx) and x (dW) may be NULL too.  dz is rounded to
- * dtype once, as the operand of the two products; dbias sums it unrounded.
+ * dtype once, as the operand of the two products (in small layers, of up to
+ * 2^22 products and 1024 terms of a sum, not at all); dbias sums it unrounded.
  * The residual's gradient is dy itself.  x must have been stored in dtype.  A
  * group of x that holds a non-finite value makes its column of dW NaN.
  * M == 0 gives zero dW and dbias. */
@@ -354,7 +358,10 @@ int trellis_dense(const uint32_t *packed, int64_t B, const float *codebook, int 
 /* qat_linear_act with W [N, K] given by its paths: packed [N, K / block,
  * words], row n's weights block by block, times scales [N, K / block] if
  * given.  K must be a multiple of block.  The weights are rounded to dtype
- * (before or after their scale) as the matrix instructions' operands.
+ * (before or after their scale, so the codebook's values must lie in dtype's
+ * range too) as the matrix instructions' operands; up to 16 tokens through few
+ * weights multiply them in fp32.  An infinity in x makes its token's outputs
+ * infinite or NaN.
  * Workspace: trellis_linear_workspace_bytes() bytes, 16-byte aligned. */
 size_t trellis_linear_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K, int state_bits, int k,
                                       int V, int64_t block);

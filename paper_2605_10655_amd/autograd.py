@@ -22,6 +22,8 @@ the checkpoint's z; everything else is exact up to rounding.
 """
 from __future__ import annotations
 
+import weakref
+
 import torch
 
 from . import bcjr_soft_codeword, bcjr_soft_codeword_vjp, bcjr_ste_vjp, viterbi_decode
@@ -82,11 +84,33 @@ def bcjr_quant(W, codebook, state_bits: int, k: int, T, block: int = 256, hard: 
     return out.reshape(W.shape)
 
 
+# LinearAct8's nodes of graphs recorded eagerly on a device's default stream.
+_EAGER = weakref.WeakSet()
+
+
+def _note_leaves(ctx, tensors):
+    """Refuses to capture a layer while an eager graph over the same leaves
+    lives.  The leaf's gradient is accumulated on the stream that the older
+    graph was recorded on; where that is the default stream, a captured
+    backward pass would order it behind the capture, which ends the process."""
+    ids = frozenset(id(t) for t, need in zip(tensors, ctx.needs_input_grad) if need and t.is_leaf)
+    if not ids:
+        return
+    if torch.cuda.is_current_stream_capturing():
+        if any(not ids.isdisjoint(node.leaves) for node in list(_EAGER)):
+            raise RuntimeError("linear_act8 is being captured while the result of an eager call on the same "
+                               "leaves lives: drop that result first, or run it on a stream of its own")
+    elif torch.cuda.current_stream(tensors[0].device).cuda_stream == 0:
+        ctx.leaves = ids
+        _EAGER.add(ctx)
+
+
 class LinearAct8(torch.autograd.Function):
     """activation(x W^T + bias) + residual with 8-bit checkpoints."""
 
     @staticmethod
     def forward(ctx, x, W, bias, residual, activation, x8):
+        _note_leaves(ctx, (x, W, bias, residual))
         need_x, need_W, need_b, need_r = ctx.needs_input_grad[:4]
         need_z = activation != "none" and (need_x or need_W or need_b)
         out = linear_act(x, W, bias, residual, activation, save=need_z)
@@ -116,11 +140,15 @@ def linear_act8(x, W, bias=None, residual=None, activation="none", x8=None):
     """activation(x W^T + bias) + residual, x [..., K], W [N, K] (float32,
     bfloat16 or float16, one type for all), differentiable in all four; the
     backward pass reads x and x W^T + bias in 8 bits.  x8: the checkpoint
-    act8_store(x), where several layers read the same x."""
+    act8_store(x), where several layers read the same x.  Captured into a graph
+    it is refused while the result of an eager call on the default stream, with
+    a leaf in common, is kept."""
     if x8 is not None:
         if not isinstance(x8, Act8):
             raise TypeError("x8 must be an Act8")
         rows = x.numel() // max(x.shape[-1], 1)
         if (x8.rows, x8.cols, x8.dtype) != (rows, x.shape[-1], x.dtype):
             raise ValueError("x8 is not a checkpoint of x: its size or type differs")
+    if not torch.is_grad_enabled():   # nothing to keep for a backward pass
+        return linear_act(x, W, bias, residual, activation)
     return LinearAct8.apply(x, W, bias, residual, activation, x8)

@@ -15,8 +15,9 @@ inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+// a launch has fewer than 2^32 threads along an axis
+inline bool grid_fits(int64_t groups, int threads) { return groups < ((int64_t)1 << 32) / threads; }
 inline int launched() { return hipGetLastError() == hipSuccess ? BCJR_OK : BCJR_ERR_HIP; }
-
 
 inline dim3 group_grid(int64_t rows, int64_t cols, int threads) {
   return dim3((unsigned)ceil_div(rows, kRows), (unsigned)ceil_div(cols, threads));
@@ -85,7 +86,9 @@ int gemm(GemmArgs g, void* ws, hipStream_t stream) {
   if (g.I == 0 || g.J == 0) return BCJR_OK;
   constexpr int es = (int)sizeof(T), dtype = es == 4 ? kF32 : kBF16;
   GemmPlan p = gemm_plan(dtype, g.I, g.J, g.K);
-  if ((int64_t)p.ti * p.tj * 4 * p.splits >= ((int64_t)1 << 31)) return BCJR_ERR_UNSUPPORTED;   // one grid
+  // (without copies a tile of 256 becomes four workgroups of 256 threads)
+  if (!grid_fits((int64_t)p.ti * p.tj * p.splits, p.tile == 256 ? 1024 : p.tile == 128 ? 512 : 256))
+    return BCJR_ERR_UNSUPPORTED;
   g.splits = p.splits;
   g.part = static_cast<float*>(ws);
   if (copies(AM, g.a, g.lda, g.I, g.K, es, p.tile) && copies(BM, g.b, g.ldb, g.J, g.K, es, p.tile)) {

@@ -41,7 +41,7 @@ bool dtype_ok(int dtype) { return dtype == kF32 || dtype == kBF16 || dtype == kF
 bool act_ok(int act) { return act >= kActNone && act <= kActGeluTanh; }
 bool dims_ok(int64_t M, int64_t N, int64_t K) { return M >= 0 && N >= 1 && K >= 1; }
 // a tile's rows stay within 32-bit offsets
-bool strides_fit(int64_t a, int64_t b, size_t es) { return a * (int64_t)es < (1 << 25) && b * (int64_t)es < (1 << 25); }
+bool strides_fit(int64_t a, int64_t b, size_t es) { return a < (1 << 25) / (int64_t)es && b < (1 << 25) / (int64_t)es; }
 bool dims_fit(int64_t M, int64_t N, int64_t K) { return M < kMaxRows && N < kMaxCols && K < kMaxCols; }
 template <class F>
 int by_type(int dtype, F f) {
@@ -55,9 +55,9 @@ dim3 band_grid(int64_t rows, int64_t cols) {
   return dim3((unsigned)(ceil_div(rows, kRows) * ceil_div(cols, kGroupThreads * kCols<T>)));
 }
 
-// workgroups of 32 rows and at least 256 columns that one launch can have
-bool bands_fit(int64_t rows, int64_t cols) {
-  return ceil_div(rows, kRows) * ceil_div(cols, kGroupThreads) < ((int64_t)1 << 31);
+bool bands_fit(int dtype, int64_t rows, int64_t cols) {
+  const int64_t wide = kGroupThreads * (dtype == kF32 ? kCols<float> : kCols<bf16>);
+  return grid_fits(ceil_div(rows, kRows) * ceil_div(cols, wide), kGroupThreads);
 }
 
 int run_linear(const GemmArgs& g, int dtype, void* ws, hipStream_t stream) {
@@ -176,8 +176,7 @@ bool small_codes(const Code& c, int64_t M, int64_t N, int64_t K) {
   return !codes_take(c.k, c.V, c.block, M, N, K) || N * K <= (table > few ? table : few);
 }
 
-// blocks of 256 threads that one launch can have
-bool threads_fit(int64_t n) { return ceil_div(n, 256) < ((int64_t)1 << 31); }
+bool threads_fit(int64_t n) { return grid_fits(ceil_div(n, 256), 256); }
 
 }  // namespace
 }  // namespace qlin
@@ -190,7 +189,7 @@ extern "C" {
 int qat_act8_store(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t* codes,
                    uint16_t* scales, hipStream_t stream) {
   if (!dtype_ok(dtype) || rows < 0 || cols < 1 || ldx < cols) return BCJR_ERR_INVALID_ARG;
-  if (rows >= kMaxRows || cols >= kMaxCols || !bands_fit(rows, cols)) return BCJR_ERR_UNSUPPORTED;
+  if (rows >= kMaxRows || cols >= kMaxCols || !bands_fit(dtype, rows, cols)) return BCJR_ERR_UNSUPPORTED;
   if (rows == 0) return BCJR_OK;
   if (!x || !codes || !scales || misaligned(x, elem_size(dtype)) || misaligned(codes, 16) || misaligned(scales, 2))
     return BCJR_ERR_INVALID_ARG;
@@ -205,7 +204,7 @@ int qat_act8_store(const void* x, int dtype, int64_t rows, int64_t cols, int64_t
 int qat_act8_load(const int8_t* codes, const uint16_t* scales, int64_t rows, int64_t cols, void* out, int dtype,
                   int64_t ldo, hipStream_t stream) {
   if (!dtype_ok(dtype) || rows < 0 || cols < 1 || ldo < cols) return BCJR_ERR_INVALID_ARG;
-  if (rows >= kMaxRows || cols >= kMaxCols || !bands_fit(rows, cols)) return BCJR_ERR_UNSUPPORTED;
+  if (rows >= kMaxRows || cols >= kMaxCols || !bands_fit(dtype, rows, cols)) return BCJR_ERR_UNSUPPORTED;
   if (rows == 0) return BCJR_OK;
   if (!out || !codes || !scales || misaligned(out, elem_size(dtype)) || misaligned(codes, 16) ||
       misaligned(scales, 2))
@@ -255,7 +254,7 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
   if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || ldd < N || (dx && ldw < K))
     return BCJR_ERR_INVALID_ARG;
   const size_t es = elem_size(dtype);
-  if (!dims_fit(M, N, K) || !bands_fit(M, N) || !strides_fit(ldd, dx ? ldw : 1, es)) return BCJR_ERR_UNSUPPORTED;
+  if (!dims_fit(M, N, K) || !bands_fit(dtype, M, N) || !strides_fit(ldd, dx ? ldw : 1, es)) return BCJR_ERR_UNSUPPORTED;
   if (!dx && !dW && !dbias) return BCJR_OK;
   if (misaligned(dy, es) || misaligned(W, es) || misaligned(dx, es) || misaligned(dW, es) || misaligned(dbias, es) ||
       misaligned(x_codes, 16) || misaligned(z_codes, 16) || misaligned(x_scales, 2) || misaligned(z_scales, 2))

@@ -625,6 +625,122 @@ def test_autograd_gives_the_calls_gradients():
         linear_act8(devi[0][:3], devi[1], x8=x8)
 
 
+def _padded_layer():
+    _, (x, W, b, r) = _layer(5, 96, 40, 64, torch.bfloat16)
+    return x, W, b, r
+
+
+def test_training_step_replays():
+    """Forward and backward of two layers captured together, with new inputs
+    between eager steps over other leaves of the same values."""
+    x, W, b, r = _padded_layer()
+    dy = torch.randn(96, 40, generator=torch.Generator().manual_seed(3)).bfloat16().cuda()
+
+    def step(x, leaves):
+        h = linear_act8(x, leaves[0], leaves[1], None, "gelu")
+        y = linear_act8(h, leaves[2], None, r, "silu")
+        return (y, *torch.autograd.grad(y, leaves, dy))
+
+    def leaves():
+        g = torch.Generator().manual_seed(4)
+        return [t.clone().requires_grad_() for t in (W, b, torch.randn(40, 40, generator=g).bfloat16().cuda())]
+
+    static = leaves()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(x, static)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(x, static)
+    for i in range(4):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(i)))
+        want = [t.clone() for t in step(x, leaves())]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, w) for a, w in zip(out, want)), i
+
+
+def test_capture_over_the_leaves_of_a_living_graph_is_refused(monkeypatch):
+    """Without a capture: what the call asks of the stream is answered here."""
+    x, W, b, r = _padded_layer()
+    W, b = W.requires_grad_(), b.requires_grad_()
+    y = linear_act8(x, W, b, r, "gelu")
+    z = linear_act8(x, W.detach().clone().requires_grad_())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    for leaf in (dict(bias=b), dict()):
+        with pytest.raises(RuntimeError):
+            linear_act8(x, W, **leaf)
+    with pytest.raises(RuntimeError):
+        linear_act8(x, W.detach(), b)
+    linear_act8(x, W.detach(), b.detach())            # no leaf
+    with torch.no_grad():
+        linear_act8(x, W, b)
+    kept = linear_act8(x, W.detach().clone().requires_grad_())   # another
+    y.sum()
+    del y
+    assert linear_act8(x, W, b) is not None and kept is not None and z is not None
+
+
+def test_no_gradient_keeps_no_checkpoint(monkeypatch):
+    x, W, b, r = _padded_layer()
+    W = W.requires_grad_()
+    import paper_2605_10655_amd.autograd as A
+    monkeypatch.setattr(A, "act8_store", None)   # not called
+    with torch.no_grad():
+        assert torch.equal(linear_act8(x, W, b, r, "gelu"), Q.linear_act(x, W.detach(), b, r, "gelu"))
+    with pytest.raises(TypeError):
+        linear_act8(x, W, b, r, "gelu")
+
+
+def test_same_tensors_twice_and_views():
+    """One tensor as several operands, overlapping views as inputs, and a
+    batch whose padding rows hold NaN."""
+    g = torch.Generator().manual_seed(9)
+    a = torch.randn(48, 48, generator=g).cuda()
+    y = Q.linear_act(a, a, a[0].contiguous(), a, "silu")
+    assert torch.equal(y, Q.linear_act(a.clone(), a.clone(), a[0].clone(), a.clone(), "silu"))
+    x = a[:40]
+    assert torch.equal(Q.linear_act(x, a[8:]), Q.linear_act(x.clone(), a[8:].clone()))
+    x8 = Q.act8_store(a)
+    one = Q.linear_act_vjp(a, x8, a, Q.act8_store(a), "gelu")
+    two = Q.linear_act_vjp(a.clone(), Q.act8_store(a.clone()), a.clone(), Q.act8_store(a.clone()), "gelu")
+    assert all(torch.equal(p, q) for p, q in zip(one, two))
+    for M in (16, 17, 300):
+        x, W = torch.randn(M, 64, generator=g).cuda(), torch.randn(40, 64, generator=g).cuda()
+        pad = x.clone()
+        pad[M - 3:] = float("nan")
+        assert torch.equal(Q.linear_act(pad, W, activation="gelu_tanh")[:M - 3],
+                           Q.linear_act(x, W, activation="gelu_tanh")[:M - 3])
+        assert torch.isnan(Q.linear_act(pad, W)[M - 3:]).all()
+    _, s, packed, cd, sd = _coded(2, 40, 256, 10, 2, 1, 256)
+    x = torch.randn(16, 256, generator=g).cuda()
+    pad = x.clone()
+    pad[9:] = float("nan")
+    assert torch.equal(Q.trellis_linear(pad, packed, cd, 10, 2, scales=sd)[:9],
+                       Q.trellis_linear(x, packed, cd, 10, 2, scales=sd)[:9])
+
+
+def test_two_streams_at_once():
+    """The same layer on two streams, workspaces of their own."""
+    _, (x, W, b, r) = _layer(6, 300, 264, 520, torch.bfloat16)
+    want = Q.linear_act(x, W, b, r, "gelu", save=True)
+    x8 = Q.act8_store(x)
+    grads = Q.linear_act_vjp(r, x8, W, want[1], "gelu")
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(5):
+        for s in streams:
+            y, z8 = Q.linear_act(x, W, b, r, "gelu", save=True, stream=s)
+            got.append((y, z8.codes, z8.scales, *Q.linear_act_vjp(r, x8, W, z8, "gelu", stream=s)))
+    torch.cuda.synchronize()
+    for y in got:
+        assert all(torch.equal(p, q) for p, q in zip(y, (want[0], want[1].codes, want[1].scales, *grads)))
+
+
 # ---------------------------------------------------------------- a run of them together
 def test_train_then_answer():
     """A layer trained through its soft codewords, snapped, packed and asked:

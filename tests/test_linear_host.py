@@ -62,7 +62,7 @@ def test_linear_act_arguments(lib):
 def test_vjp_arguments(lib):
     ws = lib.qat_linear_act_vjp_workspace_bytes
     assert ws(5, 4, 8, 16, 0) == 0 and ws(1, 4, 0, 16, 0) == 0 and ws(1, 4, 8, 16, 9) == 0
-    assert ws(1, 64, 8, 16, 1) >= 64 * 8 * 2 + 2 * 8 * 4
+    assert ws(1, 2048, 8, 16, 1) >= 2048 * 8 * 2 + 64 * 8 * 4
     # dy ldd xc xs W ldw zc zs dtype act M N K dx dW dbias ws bytes stream
     ok = [FAKE, 8, FAKE, FAKE, FAKE, 16, FAKE, FAKE, 1, 1, 4, 8, 16, FAKE, FAKE, FAKE, FAKE, 1 << 40, None]
     for bad in (dict(_0=None), dict(_1=7), dict(_2=None), dict(_2=FAKE + 4), dict(_3=None), dict(_4=None),
@@ -70,7 +70,7 @@ def test_vjp_arguments(lib):
                 dict(_12=0), dict(_13=FAKE + 1), dict(_14=FAKE + 1), dict(_15=FAKE + 1)):
         assert lib.qat_linear_act_vjp(*change(ok, **bad)) == INVALID, bad
     for bad in (dict(_16=None), dict(_16=FAKE + 8), dict(_17=16)):
-        assert lib.qat_linear_act_vjp(*change(ok, **bad)) == WORKSPACE, bad
+        assert lib.qat_linear_act_vjp(*change(ok, _10=2048, **bad)) == WORKSPACE, bad
     assert lib.qat_linear_act_vjp(*change(ok, _13=None, _14=None, _15=None)) == 0
     assert lib.qat_linear_act_vjp(*change(ok, _12=1 << 22, _5=1 << 22)) == UNSUPPORTED
 
@@ -106,8 +106,43 @@ def test_trellis_arguments(lib):
                 dict(_14=-1), dict(_15=0), dict(_17=None), dict(_18=7)):
         assert lib.trellis_linear(*change(ok, **bad)) == INVALID, bad
     for bad in (dict(_19=None), dict(_19=FAKE + 8), dict(_20=16)):
-        assert lib.trellis_linear(*change(ok, **bad)) == WORKSPACE, bad
+        assert lib.trellis_linear(*change(ok, _14=17, **bad)) == WORKSPACE, bad
     assert lib.trellis_linear(*change(ok, _14=0)) == 0
+
+
+def test_launches_and_strides_past_the_limits(lib):
+    """Grids of 2^32 threads and rows further apart than 32-bit offsets reach."""
+    top = (1 << 31) - 1
+    for dtype in (0, 1, 2):
+        es = 4 if dtype == 0 else 2
+        wide = 64 * (1 if dtype == 0 else 2)     # columns of a workgroup of 64 threads and 32 rows
+        assert lib.qat_act8_store(FAKE, dtype, top, wide, wide, FAKE, FAKE, None) == UNSUPPORTED
+        assert lib.qat_act8_load(FAKE, FAKE, top, wide, FAKE, dtype, wide, None) == UNSUPPORTED
+        far = (1 << 25) // es
+        for ldx, ldw in ((far, 16), (16, far), (1 << 62, 16), (16, 1 << 62)):
+            assert lib.qat_linear_act(FAKE, ldx, FAKE, ldw, None, None, 0, dtype, 0, 4, 8, 16, FAKE, 8, None, None,
+                                      FAKE, 1 << 40, None) == UNSUPPORTED
+            assert lib.qat_linear_act_vjp(FAKE, ldx, FAKE, FAKE, FAKE, ldw, None, None, dtype, 0, 4, 8, 16, FAKE,
+                                          FAKE, FAKE, FAKE, 1 << 40, None) == UNSUPPORTED
+        assert lib.trellis_linear(FAKE, far, FAKE, FAKE, 8, 2, 1, 16, None, None, None, 0, dtype, 0, 4, 8, 16, FAKE,
+                                  8, FAKE, 1 << 40, None) == UNSUPPORTED
+        # tiles of 64 rows by 256 threads
+        assert lib.qat_linear_act(FAKE, 8, FAKE, 8, None, None, 0, dtype, 0, 1 << 30, 8, 8, FAKE, 8, None, None,
+                                  FAKE, 1 << 40, None) == UNSUPPORTED
+    assert lib.trellis_unpack(FAKE, 1 << 24, 256, 8, 2, FAKE, None) == UNSUPPORTED
+    assert lib.trellis_dense(FAKE, 1 << 24, FAKE, 8, 2, 1, 256, None, FAKE, 0, None) == UNSUPPORTED
+
+
+def test_small_layers_need_no_workspace(lib):
+    need = lib.qat_linear_act_vjp_workspace_bytes
+    assert need(1, 64, 256, 256, 1) == 0 and need(1, 64, 256, 257, 1) > 0
+    assert need(1, 1024, 8, 8, 1) == 0 and need(1, 1025, 8, 8, 1) > 0 and need(1, 8, 1025, 8, 1) > 0
+    need = lib.trellis_linear_workspace_bytes
+    # dtype M N K state_bits k V block
+    assert need(1, 16, 1024, 1024, 12, 2, 1, 128) == 0 and need(1, 17, 1024, 1024, 12, 2, 1, 128) > 0
+    assert need(1, 16, 1032, 1024, 12, 2, 1, 128) > 0 and need(1, 1, 1, 16384, 12, 2, 1, 128) > 0
+    assert need(1, 16, 4096, 4096, 12, 2, 1, 256) == 0 and need(1, 64, 2048, 2048, 12, 2, 1, 256) == 0
+    assert need(1, 17, 4096, 4096, 12, 2, 1, 256) > 0 and need(1, 65, 256, 256, 12, 2, 1, 256) > 0
 
 
 def test_host_tensors_are_refused(lib):
