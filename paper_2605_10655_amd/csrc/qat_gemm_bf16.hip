@@ -1,5 +1,6 @@
 // qat_gemm_bf16.hip -- the products of qat_gemm_launch.h in bf16: forward (row,
-// row), gradient of x (row, col), gradient of W (col, codes).
+// row), gradient of x (row, col), gradient of W (col, codes; large ones
+// col, col).
 #include <hip/hip_runtime.h>
 
 #include "qat_gemm_launch.h"
@@ -10,6 +11,7 @@ namespace qlin {
 template int gemm<bf16, kRow, kRow>(GemmArgs, void*, hipStream_t);
 template int gemm<bf16, kRow, kCol>(GemmArgs, void*, hipStream_t);
 template int gemm<bf16, kCol, kCodes>(GemmArgs, void*, hipStream_t);
+template int gemm_large<bf16, kCol, kCol>(GemmArgs, const GemmPlan&, void*, hipStream_t);
 
 }  // namespace qlin
 }  // namespace bcjr

@@ -673,7 +673,7 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
 }
 
 // The same for large products: 256 x 256 of C per workgroup of eight waves, 128
-// x 64 of them per wave, A always copied.
+// x 64 of them per wave, both operands always copied.
 //
 // A step's 128 bytes of k are multiplied in two halves: first the upper 64 rows
 // of each wave's part, then the lower 64 with the operands of B kept in
@@ -686,7 +686,7 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
 //
 // A half has a reading and a multiplying turn, and the second four waves run
 // one turn behind the first: while one wave of a SIMD multiplies, the other
-// reads its operands from LDS, starts copies and turns codes into T.  The turn
+// reads its operands from LDS and starts copies.  The turn
 // before the first waves read a tile is a reading one of the second four's: by
 // its end every wave has seen its copies of that tile land.
 template <class T, int AM, int BM>
@@ -695,7 +695,6 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
   using TA = Tile<T, AM, 128, kThreads, 64, 128>;   // half h: rows 64 h of every 128
   using TB = Tile<T, BM, 256, kThreads>;
   using V = typename Vec<T>::type;
-  constexpr bool kCopyB = BM != kCodes;
   // tiles of their own names (see gemm_kernel)
   __shared__ __align__(16) V up0[TA::kChunks];
   __shared__ __align__(16) V up1[TA::kChunks];
@@ -724,17 +723,18 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
   const int64_t first = all * p.part / g.splits;
   const int steps = (int)(all * (p.part + 1) / g.splits - first);
   V fa[4][2], fb[4][NJ];
+  int at = lane;
   auto read_a = [&](const V* a) __attribute__((always_inline)) {
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-      for (int x = 0; x < 2; ++x) fa[kk][x] = TA::operand(a, wi / 2 + 32 * x, kk, lane);
+      for (int x = 0; x < 2; ++x) fa[kk][x] = TA::operand(a, wi / 2 + 32 * x, kk, at);
   };
   auto read_b = [&](const V* b) __attribute__((always_inline)) {
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-      for (int y = 0; y < NJ; ++y) fb[kk][y] = TB::operand(b, wj + 32 * y, kk, lane);
+      for (int y = 0; y < NJ; ++y) fb[kk][y] = TB::operand(b, wj + 32 * y, kk, at);
   };
   auto multiply = [&](auto half) __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
@@ -748,17 +748,11 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
   };
   // (a lower half past the last row reads from the first)
   const int64_t il = i0 + 64 < g.I ? i0 + 64 : i0;
-  typename TB::Regs rb;
   if (g.K % TA::kStep && p.part == g.splits - 1) {
     const int64_t k0 = all * TA::kStep;
     TA::copy_rest(g.a, g.lda, g.I, g.K, i0, k0, up0, tid);
     TA::copy_rest(g.a, g.lda, g.I, g.K, il, k0, low0, tid);
-    if constexpr (kCopyB) {
-      TB::copy_rest(g.b, g.ldb, g.J, g.K, j0, k0, b0, tid);
-    } else {
-      TB::fetch(g.b, g.ldb, g.bscales, g.J, g.K, j0, k0, rb, tid);
-      TB::put(rb, b0, tid);
-    }
+    TB::copy_rest(g.b, g.ldb, g.J, g.K, j0, k0, b0, tid);
     wait_copies<0>();
     lds_barrier();
     read_b(b0);
@@ -771,21 +765,15 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
   if (steps > 0) {
     typename TA::Copy cu, cl;
     typename TB::Copy cb;
-    typename TB::Codes codes;
     TA::start(cu, g.a, g.lda, g.I, i0, first * TA::kStep, tid);
     TA::start(cl, g.a, g.lda, g.I, il, first * TA::kStep, tid);
-    if constexpr (kCopyB)
-      TB::start(cb, g.b, g.ldb, g.J, j0, first * TA::kStep, tid);
-    else
-      TB::start_codes(codes, g.b, g.bscales, g.J, j0, first * TA::kStep, tid);
+    TB::start(cb, g.b, g.ldb, g.J, j0, first * TA::kStep, tid);
     // Copies of step s; past the last they fetch that one again, into tiles
     // that nothing reads any more, so that no turn has a branch (with branches
     // for the end in it a step took 3200 cycles, without them 2360).
     auto copy_upper = [&](int s, V* up, V* b) __attribute__((always_inline)) {
-      if constexpr (kCopyB) {
-        TB::copy(cb, b, tid);
-        cb.base += s + 1 < steps ? cb.step : 0;
-      }
+      TB::copy(cb, b, tid);
+      cb.base += s + 1 < steps ? cb.step : 0;
       TA::copy(cu, up, tid);
       cu.base += s + 1 < steps ? cu.step : 0;
     };
@@ -793,25 +781,14 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
       TA::copy(cl, lo, tid);
       cl.base += s + 1 < steps ? cl.step : 0;
     };
-    // Codes: one step's under way.  (The fences keep their loads younger than
-    // the copies before them.)
-    auto fetch = [&](int s) __attribute__((always_inline)) {
-      if constexpr (!kCopyB) {
-        asm volatile("" ::: "memory");
-        TB::fetch_all(codes, rb);
-        asm volatile("" ::: "memory");
-        codes.base += s + 1 < steps ? codes.step * kRows : 0;
-        codes.sbase += s + 1 < steps ? codes.step * 2 : 0;
-      }
-    };
-    auto put = [&](V* b) __attribute__((always_inline)) {
-      if constexpr (!kCopyB) TB::put(rb, b, tid);
-    };
     // What may be under way when the next turn's tiles have landed: all of one
-    // step's copies and one step's codes.
-    constexpr int kNew = 2 * TA::kPer + (kCopyB ? TB::kPer : TB::kLoads);
-    // Step s in the tiles up, lo, b; the other parity's are lo2 and b2.
-    auto step = [&](int s, V* up, V* lo, V* b, V* lo2, V* b2) __attribute__((always_inline)) {
+    // step's copies.
+    constexpr int kNew = 2 * TA::kPer + TB::kPer;
+    // Step s in the tiles up, lo, b; the other parity's lower one is lo2.
+    auto step = [&](int s, V* up, V* lo, V* b, V* lo2) __attribute__((always_inline)) {
+      // (fp32 columns: the addresses, worked out before the loop, would not leave
+      // the values registers enough; spilled, 8192 cubed took 14.5 ms, not 8.3)
+      if (AM == kCol && sizeof(T) == 4) asm volatile("" : "+v"(at));
       read_b(b);
       read_a(up);
       // step s - 1's lower half has been read by every wave
@@ -822,28 +799,23 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
       lds_barrier();
       // this step's B and upper half have
       copy_upper(s + 2, up, b);
-      put(b2);
-      fetch(s + 2);
       read_a(lo);
       wait_copies<kNew>();
       lds_barrier();
       multiply(Half<1>());
       lds_barrier();
     };
-    fetch(0);
-    put(b0);
     copy_upper(0, up0, b0);
     copy_lower(0, low0);
     copy_upper(1, up1, b1);
-    fetch(1);
     wait_copies<kNew>();
     lds_barrier();
     if (behind) lds_barrier();
 #pragma unroll 1
     for (int s = 0; s < steps; s += 2) {
-      step(s, up0, low0, b0, low1, b1);
+      step(s, up0, low0, b0, low1);
       if (s + 1 == steps) break;
-      step(s + 1, up1, low1, b1, low0, b0);
+      step(s + 1, up1, low1, b1, low0);
     }
     if (!behind) lds_barrier();
     wait_copies<0>();

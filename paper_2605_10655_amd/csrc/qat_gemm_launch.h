@@ -80,46 +80,57 @@ inline bool copies(int mode, const void* p, int64_t ld, int64_t rows, int64_t K,
          (int64_t)(mode == kRow ? tile : 8 * e) * ld * es < ((int64_t)1 << 31);
 }
 
+// The epilogue of a split product.
+template <class T>
+int join(const GemmArgs& g, hipStream_t stream) {
+  if (g.zcodes)
+    hipLaunchKernelGGL((join_kernel<T, true>), group_grid(g.I, g.J, 32), dim3(256), 0, stream, g);
+  else
+    hipLaunchKernelGGL((join_kernel<T, false>), dim3((unsigned)g.I, (unsigned)ceil_div(g.J, 256)), dim3(256), 0,
+                       stream, g);
+  return launched();
+}
+
+// A product that gemm_plan gives tiles of 256, of operands that can be copied.
+template <class T, int AM, int BM>
+int gemm_large(GemmArgs g, const GemmPlan& p, void* ws, hipStream_t stream) {
+  g.splits = p.splits;
+  g.part = static_cast<float*>(ws);
+  hipLaunchKernelGGL((gemm_large_kernel<T, AM, BM>), dim3((unsigned)(p.ti * p.tj * p.splits)), dim3(512), 0, stream, g,
+                     p.ti, p.tj);
+  if (launched() != BCJR_OK) return BCJR_ERR_HIP;
+  return p.splits > 1 ? join<T>(g, stream) : BCJR_OK;
+}
+
 // The product and its epilogue (of zero sums where K == 0).
 template <class T, int AM, int BM>
 int gemm(GemmArgs g, void* ws, hipStream_t stream) {
   if (g.I == 0 || g.J == 0) return BCJR_OK;
   constexpr int es = (int)sizeof(T), dtype = es == 4 ? kF32 : kBF16;
   GemmPlan p = gemm_plan(dtype, g.I, g.J, g.K);
-  // (without copies a tile of 256 becomes four workgroups of 256 threads)
-  if (!grid_fits((int64_t)p.ti * p.tj * p.splits, p.tile == 256 ? 1024 : p.tile == 128 ? 512 : 256))
+  // (a tile of 256 may become four workgroups of 512 threads)
+  if (!grid_fits((int64_t)p.ti * p.tj * p.splits, p.tile == 256 ? 2048 : p.tile == 128 ? 512 : 256))
     return BCJR_ERR_UNSUPPORTED;
+  const bool copied = copies(AM, g.a, g.lda, g.I, g.K, es, p.tile) && copies(BM, g.b, g.ldb, g.J, g.K, es, p.tile);
+  if constexpr (BM != kCodes)
+    if (copied && p.tile == 256) return gemm_large<T, AM, BM>(g, p, ws, stream);
+  if (p.tile == 256) {
+    p.ti = (int)ceil_div(g.I, 128);
+    p.tj = (int)ceil_div(g.J, 128);
+  }
   g.splits = p.splits;
   g.part = static_cast<float*>(ws);
-  if (copies(AM, g.a, g.lda, g.I, g.K, es, p.tile) && copies(BM, g.b, g.ldb, g.J, g.K, es, p.tile)) {
-    if (p.tile == 256)
-      hipLaunchKernelGGL((gemm_large_kernel<T, AM, BM>), dim3((unsigned)(p.ti * p.tj * p.splits)), dim3(512), 0, stream,
-                         g, p.ti, p.tj);
-    else if (p.tile == 128)
-      hipLaunchKernelGGL((gemm_mid_kernel<T, AM, BM>), dim3((unsigned)(p.ti * p.tj * p.splits)), dim3(512), 0, stream, g,
-                         p.ti, p.tj);
-    else
-      launch_gemm<T, AM, BM, 64, true>(g, p, stream);
-  } else {
-    if (p.tile == 256) {   // the large kernels copy A
-      p.ti = (int)ceil_div(g.I, 128);
-      p.tj = (int)ceil_div(g.J, 128);
-    }
-    if (p.tile >= 128)
-      launch_gemm<T, AM, BM, 128, false>(g, p, stream);
-    else
-      launch_gemm<T, AM, BM, 64, false>(g, p, stream);
-  }
+  if (copied && p.tile >= 128)
+    hipLaunchKernelGGL((gemm_mid_kernel<T, AM, BM>), dim3((unsigned)(p.ti * p.tj * p.splits)), dim3(512), 0, stream, g,
+                       p.ti, p.tj);
+  else if (copied)
+    launch_gemm<T, AM, BM, 64, true>(g, p, stream);
+  else if (p.tile >= 128)
+    launch_gemm<T, AM, BM, 128, false>(g, p, stream);
+  else
+    launch_gemm<T, AM, BM, 64, false>(g, p, stream);
   if (launched() != BCJR_OK) return BCJR_ERR_HIP;
-  if (p.splits > 1) {
-    if (g.zcodes)
-      hipLaunchKernelGGL((join_kernel<T, true>), group_grid(g.I, g.J, 32), dim3(256), 0, stream, g);
-    else
-      hipLaunchKernelGGL((join_kernel<T, false>), dim3((unsigned)g.I, (unsigned)ceil_div(g.J, 256)), dim3(256), 0,
-                         stream, g);
-    return launched();
-  }
-  return BCJR_OK;
+  return p.splits > 1 ? join<T>(g, stream) : BCJR_OK;
 }
 
 }  // namespace qlin
