@@ -95,7 +95,8 @@ struct Tile {
 
   // Asynchronous copy of k0 .. k0 + kStep - 1 into LDS, straight from memory:
   // needs p and ld aligned to 16 bytes, K (row) or R (col) a whole number of
-  // chunks, and a tile's span below 2 GiB.  A wave's 64 chunks go to 64
+  // chunks (or the last row's memory to go on to one), and a tile's span below
+  // 2 GiB.  A wave's 64 chunks go to 64
   // consecutive places, so each lane fetches the chunk that belongs at its
   // place: byte offsets from the tile's start, the same in every step.  Rows
   // past the end read the last one's (their sums are not stored), k past the
@@ -122,7 +123,7 @@ struct Tile {
         s.off[i] = (uint32_t)(r < last ? r : last - 1) * ldb + c * 16;
       } else {
         const int r = row_of(c * E);
-        s.off[i] = (uint32_t)line * ldb + (r < last ? r : (TO_LDS ? last - E : 0)) * (int)sizeof(T);
+        s.off[i] = (uint32_t)line * ldb + (r < last ? r : (TO_LDS ? (last - 1) / E * E : 0)) * (int)sizeof(T);
       }
     }
     const int64_t first = MODE == kRow ? r0 * ld + k0 : k0 * ld + r0;

@@ -16,9 +16,9 @@ namespace bcjr {
 namespace qlin {
 
 #define QAT_GEMM_EXTERN(T)                                                   \
-  extern template int gemm<T, kRow, kRow>(GemmArgs, void*, hipStream_t);     \
-  extern template int gemm<T, kRow, kCol>(GemmArgs, void*, hipStream_t);     \
-  extern template int gemm<T, kCol, kCodes>(GemmArgs, void*, hipStream_t);   \
+  extern template int gemm<T, kRow, kRow>(GemmArgs, void*, hipStream_t, bool);     \
+  extern template int gemm<T, kRow, kCol>(GemmArgs, void*, hipStream_t, bool);     \
+  extern template int gemm<T, kCol, kCodes>(GemmArgs, void*, hipStream_t, bool);   \
   extern template int gemm_large<T, kCol, kCol>(GemmArgs, const GemmPlan&, void*, hipStream_t);
 QAT_GEMM_EXTERN(bf16)
 QAT_GEMM_EXTERN(f16)
@@ -116,21 +116,26 @@ int run_small_vjp(SmallVjp a, hipStream_t stream) {
 
 struct VjpPlan {
   size_t dz, part, x, sums, total;
+  int64_t ldz, ldx;
   GemmPlan dW;
 };
 
 // dz, the groups' sums of dbias, x for a large dW, then the partial sums of the
 // products.  Workgroups that turn x's codes into T for themselves do it N / 256
-// times over: from tiles of 256 on x is read back once instead, where its rows
-// can then be copied (4096 tokens, 2048 x 8192, bf16: 174 us against 121 + 21).
+// times over: from tiles of 256 on x is read back once instead (4096 tokens,
+// 2048 x 8192, bf16: 174 us against 121 + 21; with tiles of 128 that costs as
+// much as it gives, 44.7 and 44.3 us for 2048 cubed, with smaller ones 5 us
+// more).  Rows of dz and x are padded to 16 bytes, for whole copies.
 VjpPlan vjp_plan(int dtype, int64_t M, int64_t N, int64_t K, int act) {
   VjpPlan p = {};
   if (small_vjp(M, N, K)) return p;
-  p.dz = act == kActNone ? 0 : align_up((size_t)(M * N) * elem_size(dtype));
+  const int es = elem_size(dtype), e = 16 / es;
+  p.ldz = ceil_div(N, e) * e;
+  p.ldx = ceil_div(K, e) * e;
+  p.dz = act == kActNone ? 0 : align_up((size_t)(M * p.ldz) * es);
   p.part = align_up((size_t)(ceil_div(M, kRows) * N) * sizeof(float));
   p.dW = gemm_plan(dtype, N, K, M);
-  const int e = 16 / elem_size(dtype);
-  p.x = p.dW.tile == 256 && N % e == 0 && K % e == 0 ? align_up((size_t)(M * K) * elem_size(dtype)) : 0;
+  p.x = p.dW.tile == 256 ? align_up((size_t)(M * p.ldx) * es) : 0;
   const size_t dx = M ? gemm_plan(dtype, M, K, N).part : 0;
   p.sums = dx > p.dW.part ? dx : p.dW.part;
   p.total = p.dz + p.part + p.x + p.sums;
@@ -290,11 +295,11 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
                           : activation == kActGelu ? dz_kernel<T, kActGelu>
                                                    : dz_kernel<T, kActGeluTanh>;
       hipLaunchKernelGGL(kernel, band_grid<T>(M, N), dim3(kGroupThreads), 0, stream, static_cast<const T*>(dy), ldd,
-                         z_codes, z_scales, M, N, reinterpret_cast<T*>(ws), dbias ? part : nullptr);
+                         z_codes, z_scales, M, N, reinterpret_cast<T*>(ws), p.ldz, dbias ? part : nullptr);
       if (launched() != BCJR_OK) return BCJR_ERR_HIP;
       if (activation != kActNone) {
         dz = reinterpret_cast<const T*>(ws);
-        ldz = N;
+        ldz = p.ldz;
       }
     }
     if (dbias) {
@@ -309,14 +314,15 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
     }
     if (dW) {
       GemmArgs g = {dz, x_codes, ldz, 0, x_scales, N, K, M, nullptr, nullptr, 0, dW, K, nullptr, nullptr, kActNone};
-      if (!p.x || !bands_fit(dtype, M, K) || !copies(kCol, dz, ldz, N, M, (int)es, 256) || !copies(kCol, x_codes, K, K, M, (int)es, 256))
-        return gemm<T, kCol, kCodes>(g, sums, stream);
+      const bool padded = activation != kActNone;
+      if (!p.x || !bands_fit(dtype, M, K) || !copies(kCol, dz, ldz, N, M, (int)es, 256, padded))
+        return gemm<T, kCol, kCodes>(g, sums, stream, padded);
       T* x = reinterpret_cast<T*>(ws + p.dz + p.part);
       hipLaunchKernelGGL(act8_load_kernel<T>, band_grid<T>(M, K), dim3(kGroupThreads), 0, stream, x_codes, x_scales, M,
-                         K, x, K);
+                         K, x, p.ldx);
       if (launched() != BCJR_OK) return BCJR_ERR_HIP;
       g.b = x;
-      g.ldb = K;
+      g.ldb = p.ldx;
       return gemm_large<T, kCol, kCol>(g, p.dW, sums, stream);
     }
     return BCJR_OK;

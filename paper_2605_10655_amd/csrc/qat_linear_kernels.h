@@ -178,7 +178,7 @@ template <class T, int ACT>
 __global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__ dy, int64_t ldd,
                                                            const int8_t* __restrict__ zcodes,
                                                            const uint16_t* __restrict__ zscales, int64_t rows,
-                                                           int64_t cols, T* __restrict__ dz,
+                                                           int64_t cols, T* __restrict__ dz, int64_t ldz,
                                                            float* __restrict__ part) {
   constexpr int C = kCols<T>;
   const Band b = band_of<C>(cols);
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__
     const int64_t r0 = b.g * kRows + 16 * h;
     float v[16][C];
     get_rows<T, C, 16>(dy + r0 * ldd + b.c, ldd, left - 16 * h, b.n, v);
-    T* dst = dz + r0 * cols + b.c;
+    T* dst = dz + r0 * ldz + b.c;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       if (ACT != kActNone) {
@@ -210,7 +210,7 @@ __global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__
         for (int c = 0; c < C; ++c) v[i][c] = scaled(act_slope(q8_value(code_at(&w[c][h], i), s[c]), ACT), v[i][c]);
       }
       if (16 * h + i < left) {
-        if (ACT != kActNone) set<T, C>(dst + i * cols, b.n, v[i]);
+        if (ACT != kActNone) set<T, C>(dst + i * ldz, b.n, v[i]);
 #pragma unroll
         for (int c = 0; c < C; ++c) eights[2 * h + i / 8][c] += v[i][c];
       }
