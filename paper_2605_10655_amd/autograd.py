@@ -94,7 +94,7 @@ def _note_leaves(ctx, tensors):
     graph was recorded on; where that is the default stream, a captured
     backward pass would order it behind the capture, which ends the process."""
     ids = frozenset(id(t) for t, need in zip(tensors, ctx.needs_input_grad) if need and t.is_leaf)
-    if not ids:
+    if not ids or not tensors[0].is_cuda:   # (linear_act refuses the latter)
         return
     if torch.cuda.is_current_stream_capturing():
         if any(not ids.isdisjoint(node.leaves) for node in list(_EAGER)):

@@ -133,7 +133,7 @@ VjpPlan vjp_plan(int dtype, int64_t M, int64_t N, int64_t K, int act) {
   p.ldz = ceil_div(N, e) * e;
   p.ldx = ceil_div(K, e) * e;
   p.dz = act == kActNone ? 0 : align_up((size_t)(M * p.ldz) * es);
-  p.part = align_up((size_t)(ceil_div(M, kRows) * N) * sizeof(float));
+  p.part = align_up((size_t)(2 * ceil_div(M, kRows) * N) * sizeof(float));
   p.dW = gemm_plan(dtype, N, K, M);
   p.x = p.dW.tile == 256 ? align_up((size_t)(M * p.ldx) * es) : 0;
   const size_t dx = M ? gemm_plan(dtype, M, K, N).part : 0;
@@ -267,7 +267,7 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
   if (!dtype_ok(dtype) || !act_ok(activation) || !dims_ok(M, N, K) || ldd < N || (dx && ldw < K))
     return BCJR_ERR_INVALID_ARG;
   const size_t es = elem_size(dtype);
-  if (!dims_fit(M, N, K) || !bands_fit(dtype, M, N) || !strides_fit(ldd, dx ? ldw : 1, es)) return BCJR_ERR_UNSUPPORTED;
+  if (!dims_fit(M, N, K) || !bands_fit(dtype, 2 * M, N) || !strides_fit(ldd, dx ? ldw : 1, es)) return BCJR_ERR_UNSUPPORTED;
   if (!dx && !dW && !dbias) return BCJR_OK;
   if (misaligned(dy, es) || misaligned(W, es) || misaligned(dx, es) || misaligned(dW, es) || misaligned(dbias, es) ||
       misaligned(x_codes, 16) || misaligned(z_codes, 16) || misaligned(x_scales, 2) || misaligned(z_scales, 2))
@@ -294,7 +294,8 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
                           : activation == kActSilu ? dz_kernel<T, kActSilu>
                           : activation == kActGelu ? dz_kernel<T, kActGelu>
                                                    : dz_kernel<T, kActGeluTanh>;
-      hipLaunchKernelGGL(kernel, band_grid<T>(M, N), dim3(kGroupThreads), 0, stream, static_cast<const T*>(dy), ldd,
+      const dim3 grid(2 * band_grid<T>(M, N).x);   // halves of groups
+      hipLaunchKernelGGL(kernel, grid, dim3(kGroupThreads), 0, stream, static_cast<const T*>(dy), ldd,
                          z_codes, z_scales, M, N, reinterpret_cast<T*>(ws), p.ldz, dbias ? part : nullptr);
       if (launched() != BCJR_OK) return BCJR_ERR_HIP;
       if (activation != kActNone) {

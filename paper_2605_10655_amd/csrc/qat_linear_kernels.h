@@ -22,9 +22,8 @@ struct Band {
 };
 
 template <int C>
-__device__ __forceinline__ Band band_of(int64_t cols) {
+__device__ __forceinline__ Band band_of(int64_t cols, uint32_t id = blockIdx.x) {
   const uint32_t per = (uint32_t)((cols + kGroupThreads * C - 1) / (kGroupThreads * C));
-  const uint32_t id = blockIdx.x;
   Band b;
   b.g = id / per;
   b.c = ((int64_t)(id % per) * kGroupThreads + threadIdx.x) * C;
@@ -171,55 +170,55 @@ __global__ __launch_bounds__(kGroupThreads) void act8_load_kernel(const int8_t* 
 
 // ---------------------------------------------------------------- backward
 // dz = dy * act'(z8), rounded to T for the matrix instructions (half a step of
-// the type each, as dy itself), and the sum of the unrounded dz over each
-// group's rows.  Small layers have dz and these sums by themselves, by the same
-// operations in the same order: dbias does not depend on what else is wanted.
+// the type each, as dy itself), and the sums of the unrounded dz over 16 rows,
+// half a group each.  A workgroup takes the half: with whole groups 4096 x 2048
+// had eight waves a CU (17.5 us against 16.6; the derivative's 40 instructions
+// a value take 9, the bytes 8.5).  Small
+// layers have dz and these sums by themselves, by the same operations in the
+// same order: dbias does not depend on what else is wanted.
 template <class T, int ACT>
 __global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__ dy, int64_t ldd,
                                                            const int8_t* __restrict__ zcodes,
                                                            const uint16_t* __restrict__ zscales, int64_t rows,
                                                            int64_t cols, T* __restrict__ dz, int64_t ldz,
                                                            float* __restrict__ part) {
-  constexpr int C = kCols<T>;
-  const Band b = band_of<C>(cols);
+  constexpr int C = kCols<T>, kHalf = kRows / 2;
+  const int h = blockIdx.x & 1;
+  const Band b = band_of<C>(cols, blockIdx.x >> 1);
   if (b.n == 0) return;
-  const int64_t at = b.g * cols + b.c;
-  const int left = rows - b.g * kRows < kRows ? (int)(rows - b.g * kRows) : kRows;
-  float eights[4][C] = {};   // sums of eight rows
-  u32x4 w[C][2];
-  uint16_t s[C];
-  if (ACT != kActNone)
+  const int64_t at = b.g * cols + b.c, r0 = b.g * kRows + kHalf * h;
+  const int left = (int)(rows - r0 < kHalf ? rows - r0 : kHalf);   // 0 or less: none
+  float eights[2][C] = {};   // sums of eight rows
+  if (left > 0) {
+    u32x4 w[C];
+    uint16_t s[C];
+    if (ACT != kActNone)
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int64_t o = at + (c < b.n ? c : 0);
-      s[c] = zscales[o];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) w[c][h] = reinterpret_cast<const u32x4*>(zcodes + o * kRows)[h];
-    }
-  // 16 rows at a time: their loads together, then their products
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int64_t r0 = b.g * kRows + 16 * h;
-    float v[16][C];
-    get_rows<T, C, 16>(dy + r0 * ldd + b.c, ldd, left - 16 * h, b.n, v);
+      for (int c = 0; c < C; ++c) {
+        const int64_t o = at + (c < b.n ? c : 0);
+        s[c] = zscales[o];
+        w[c] = reinterpret_cast<const u32x4*>(zcodes + o * kRows)[h];
+      }
+    float v[kHalf][C];
+    get_rows<T, C, kHalf>(dy + r0 * ldd + b.c, ldd, left, b.n, v);
     T* dst = dz + r0 * ldz + b.c;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < kHalf; ++i) {
       if (ACT != kActNone) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) v[i][c] = scaled(act_slope(q8_value(code_at(&w[c][h], i), s[c]), ACT), v[i][c]);
+        for (int c = 0; c < C; ++c) v[i][c] = scaled(act_slope(q8_value(code_at(&w[c], i), s[c]), ACT), v[i][c]);
       }
-      if (16 * h + i < left) {
+      if (i < left) {
         if (ACT != kActNone) set<T, C>(dst + i * ldz, b.n, v[i]);
 #pragma unroll
-        for (int c = 0; c < C; ++c) eights[2 * h + i / 8][c] += v[i][c];
+        for (int c = 0; c < C; ++c) eights[i / 8][c] += v[i][c];
       }
     }
   }
   if (part)
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      if (c < b.n) part[at + c] = (eights[0][c] + eights[1][c]) + (eights[2][c] + eights[3][c]);
+      if (c < b.n) part[(2 * b.g + h) * cols + b.c + c] = eights[0][c] + eights[1][c];
 }
 
 // The groups' sums of a column, in 64 bits and a fixed order: 16 threads take
@@ -232,7 +231,8 @@ __global__ __launch_bounds__(1024) void dbias_kernel(const float* __restrict__ p
   const int64_t c = (int64_t)blockIdx.x * 64 + lane;
   double s = 0.;
   if (c < cols)
-    for (int64_t g = row; g < groups; g += 16) s += (double)part[g * cols + c];
+    for (int64_t g = row; g < groups; g += 16)
+      s += (double)(part[2 * g * cols + c] + part[(2 * g + 1) * cols + c]);
   sums[row][lane] = s;
   __syncthreads();
   if (row == 0 && c < cols) {
