@@ -32,10 +32,13 @@ struct GemmPlan {
 };
 
 // The tile and split that a model of the kernels' times finds shortest, in
-// cycles: a step of 128 bytes of k, what a workgroup takes before and after its
-// steps, and the workgroups that run at once (each measured); the parts of a
+// cycles (of about 1.5 GHz in 16 bits and 1.1 in fp32, as they run): a step of
+// 128 bytes of k, what a workgroup takes before and after its steps, and the
+// workgroups that run at once (each measured; fp32 tiles of 64 are bound by the
+// matrix instructions, so that one a CU is quicker than two); the parts of a
 // split are written, read and joined in a launch of their own.  A part has at
-// least four steps.
+// least four steps.  us, fp32, split in two and whole: 1024 cubed 28.0 and
+// 21.5; in four and whole: 512 cubed 10.6 and 12.1.
 inline GemmPlan gemm_plan(int dtype, int64_t I, int64_t J, int64_t K) {
   struct Kind {
     int tile;
@@ -43,16 +46,18 @@ inline GemmPlan gemm_plan(int dtype, int64_t I, int64_t J, int64_t K) {
     int at_once;
   };
   static constexpr Kind half[] = {{256, 2400, 9000, 256}, {128, 750, 4000, 256}, {64, 480, 3000, 512}};
-  static constexpr Kind full[] = {{256, 8600, 12000, 256}, {128, 2300, 5000, 256}, {64, 1150, 3500, 512}};
+  static constexpr Kind full[] = {{256, 8600, 12000, 256}, {128, 2300, 5000, 256}, {64, 1150, 3500, 512}, {64, 700, 3500, 256}};
   const int64_t steps = ceil_div(K, dtype == kF32 ? 32 : 64);
   GemmPlan best = {};
   double least = 0.;
-  for (const Kind& k : dtype == kF32 ? full : half) {
+  const Kind* const kinds = dtype == kF32 ? full : half;
+  for (int n = 0; n < (dtype == kF32 ? 4 : 3); ++n) {
+    const Kind& k = kinds[n];
     const int64_t ti = ceil_div(I, k.tile), tj = ceil_div(J, k.tile), tiles = ti * tj;
     for (int64_t s = 1; s == 1 || (s <= steps / 4 && s <= 64 && tiles * s <= 2 * k.at_once); ++s) {
       const double rounds = (double)ceil_div(tiles * s, k.at_once);
       double t = rounds * ((double)ceil_div(steps, s) * k.step + k.fixed);
-      if (s > 1) t += 9000. + (double)(s * I * J) * 8. / 2000.;
+      if (s > 1) t += dtype == kF32 ? 5500. + (double)(s * I * J) / 440. : 9000. + (double)(s * I * J) / 250.;
       if (best.tile == 0 || t < least) {
         least = t;
         best.tile = k.tile;
