@@ -31,6 +31,10 @@ struct CodesArgs : FewArgs {
 // are not used, and half the rows a tile fill twice the CUs.
 //
 // Waves of a workgroup split K; their sums meet in LDS in a fixed order.
+//
+// bf16, 16 state bits: one token, 2048 -> 8192, 2 bits a weight 11.5 us (table
+// reads 3.6, filling the tables and the launch most of the rest); 16 tokens,
+// 2048 x 2048, two weights a step 14.5.
 constexpr int kChunk = 256;       // weights of a row that a wave takes at once
 
 
@@ -194,7 +198,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
 // rows of 8192, kept in registers while the fp32 codebook passes through LDS in
 // pieces of 128 KB; of each, states of the others read a zero.  (Read from L2
 // a weight costs 1.1 cycles a CU and requests 64 bytes for 4: 16.8 million
-// weights took 74 us.)
+// weights took 74 us; this takes 21, 7 of them reads of the tables.)
 constexpr int kDenseThreads = 1024, kDenseGroups = 8;
 
 template <class T, int KB, int V>

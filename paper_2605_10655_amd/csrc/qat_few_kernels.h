@@ -121,7 +121,8 @@ __device__ __forceinline__ typename Frag<T>::type eight(const T* p, int n) {
 // takes the next 16 bytes of 64 of a row, with Q = 2 (at most 8 tokens) rows
 // 8..15 are the same rows 64 bytes on, so that a load takes whole 128-byte
 // lines; tokens 8..15 are then the same tokens there, the products of unlike
-// halves are not used, and half the rows a tile fill twice the CUs.
+// halves are not used, and half the rows a tile fill twice the CUs.  bf16, one
+// token, 2048 x 8192: 8.2 us, 4.1 TB/s of weights.
 template <class T, int Q>
 __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(FewArgs a, const T* W, int64_t ldw) {
   using F = typename Frag<T>::type;

@@ -34,7 +34,8 @@ int dense_large(const uint32_t* packed, int64_t B, const float* codebook, int n,
 
 namespace {
 
-// Limits of the grids: columns of any operand lie along a grid's second axis.
+// Columns are below 2^22, so that a group's codes and a tile's offsets stay
+// below 2^31.
 constexpr int64_t kMaxRows = (int64_t)1 << 31, kMaxCols = (int64_t)1 << 22;
 
 int elem_size(int dtype) { return dtype == kF32 ? 4 : 2; }
