@@ -426,32 +426,41 @@ __device__ __forceinline__ void put_strip(T* y, int64_t ldy, const T* bias, cons
     const int row = u / kRun, col = (u % kRun) * E;
     const int64_t i = i0 + row, j = j0 + col, n = J - j;
     if (i >= I || n <= 0) continue;
+    T* out = y + i * ldy + j;
+    const T* r = res ? res + i * ldr + j : nullptr;
+    V bv, rv, o;
+#pragma unroll
+    for (int e = 0; e < E; ++e) bv[e] = rv[e] = (T)0.f;
+    if (n >= E) {
+      if (bias) __builtin_memcpy(&bv, bias + j, 16);
+      if (r) __builtin_memcpy(&rv, r, 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (bias && e < n) bv[e] = bias[j + e];
+        if (r && e < n) rv[e] = r[e];
+      }
+    }
     float v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = strip[row * (WJ + 4) + col + e];
     if (bias)
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] += e < n ? (float)bias[j + e] : 0.f;
+      for (int e = 0; e < E; ++e) v[e] += (float)bv[e];
     if (act != kActNone)
 #pragma unroll
       for (int e = 0; e < E; ++e) v[e] = act_value(v[e], act);
-    T* out = y + i * ldy + j;
-    const T* r = res ? res + i * ldr + j : nullptr;
-    V o;
+    if (r)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] += (float)rv[e];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = (T)v[e];
     if (n >= E) {
-      if (r) {
-        V rv;
-        __builtin_memcpy(&rv, r, 16);
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] += (float)rv[e];
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = (T)v[e];
       __builtin_memcpy(out, &o, 16);
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (e < n) out[e] = (T)(r ? v[e] + (float)r[e] : v[e]);
+        if (e < n) out[e] = o[e];
     }
   }
 }
