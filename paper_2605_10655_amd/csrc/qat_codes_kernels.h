@@ -73,7 +73,8 @@ __device__ __forceinline__ void fill_table(T* table, const float* codebook, int 
 }
 
 // (One workgroup fills a CU's LDS: four waves a SIMD and their 128 registers,
-// which the compiler would otherwise not all use to keep loads under way.)
+// which the compiler would otherwise not all use to keep loads under way: 16.2
+// us against 14.5 for the second of the two above.)
 template <class T, int KB, int V, int MT, int Q>
 __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(4, 4))) void codes_kernel(
     CodesArgs a) {

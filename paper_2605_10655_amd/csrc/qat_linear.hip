@@ -186,7 +186,10 @@ int launch_small(SmallCodes a, hipStream_t stream) {
 // 18.7 us in one launch, 11 in two; figures of others beside the kernel).
 bool small_codes(const Code& c, int64_t M, int64_t N, int64_t K) {
   if (M > 16 || K > 8192 || N * K > ((int64_t)1 << 20)) return false;
-  const int64_t table = (int64_t)c.V << (c.n + 4), few = (int64_t)1 << 16;
+  // a table of 2^n states against 16 and more weights a state; of a small one
+  // the fp32 product costs up to 4 tokens nothing (512 x 1024, 8 state bits: 4.2
+  // to 4.5 us against 4.0 to 4.1), 16 tokens 3 us
+  const int64_t table = (int64_t)c.V << (c.n + 4), few = (int64_t)1 << (M <= 4 ? 18 : 16);
   return !codes_take(c.k, c.V, c.block, M, N, K) || N * K <= (table > few ? table : few);
 }
 
