@@ -27,6 +27,8 @@ and the training helpers:
     bcjr_gaussian_codebook(state_bits, V, seed)                       -> codebook [S] or [S, V]
     qat_adam_step(param, grad, m, v, lr, beta1, beta2, eps, step, grad_clip)   (in place)
     qat_sgd_step(param, grad, lr, grad_clip)                          (in place)
+The linear layer that trains and answers with the codewords is in
+``paper_2605_10655_amd.linear``.
 """
 from __future__ import annotations
 
