@@ -847,20 +847,20 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
 }
 
 // For products of too few such tiles to fill the CUs: 128 x 128 of C per
-// workgroup of eight waves in turns, 64 x 32 of them per wave, A always copied.
-// A tile this size takes 64 bytes of copies a cycle at the matrix
-// instructions' full rate, which is all that a CU can fetch; four buffers keep
-// three steps of copies under way.  bf16, 2048 tokens, 8192 -> 2048: 73 us,
-// 940 TFLOP/s.
+// workgroup of eight waves in turns, A always copied, three of four buffers'
+// copies under way.  A wave takes 64 x 64 of C and half of each step's k, and
+// the halves' sums meet in LDS at the end: with 64 x 32 and all of k the operands'
+// reads took 768 cycles of LDS a step, the matrix instructions 512.  bf16, 2048
+// tokens, 8192 -> 2048: XX us, 940 TFLOP/s.
 template <class T, int AM, int BM>
 __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int tj) {
-  constexpr int kThreads = 512, BT = 128, NI = 2;
+  constexpr int kThreads = 512, BT = 128;
   using TA = Tile<T, AM, BT, kThreads>;
   using TB = Tile<T, BM, BT, kThreads>;
   using V = typename Vec<T>::type;
   constexpr bool kCopyB = BM != kCodes;
-  constexpr int kBuf = TA::kChunks + TB::kChunks, kStrip = 32 * (32 + 4);
-  static_assert(2 * kStrip * 4 <= kBuf * 16, "strips fit the buffers");
+  constexpr int kBuf = TA::kChunks + TB::kChunks, kStrip = 32 * (64 + 4), kGiven = 2 * 16 * 64;
+  static_assert(3 * kStrip * 4 <= kBuf * 16 && 4 * kGiven * 4 <= kBuf * 16, "strips and sums fit the buffers");
   __shared__ __align__(16) V lds0[kBuf];
   __shared__ __align__(16) V lds1[kBuf];
   __shared__ __align__(16) V lds2[kBuf];
@@ -869,33 +869,38 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
   const Place p = place_of(ti, tj, g.splits);
   const int64_t i0 = (int64_t)p.i * BT, j0 = (int64_t)p.j * BT;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wi = (wave >> 2) * 64, wj = (wave & 3) * 32;
-  const bool behind = wave >= 4;
-  f32x16 acc[NI][1];
+  const int wi = (wave >> 1 & 1) * 64, wj = (wave & 1) * 64;
+  const bool behind = wave >= 4;   // of the later half of k, too
+  f32x16 acc[2][2];
 #pragma unroll
-  for (int x = 0; x < NI; ++x)
+  for (int x = 0; x < 2; ++x)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[x][0][r] = 0.f;
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
 
   // Whole steps; what is left of k goes first, on its own.
   const int64_t all = g.K / TA::kStep;
   const int64_t first = all * p.part / g.splits;
   const int steps = (int)(all * (p.part + 1) / g.splits - first);
-  V fa[4][NI], fb[4];
+  V fa[2][2], fb[2][2];
   auto read = [&](const V* lds) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
+    for (int q = 0; q < 2; ++q)
 #pragma unroll
-      for (int x = 0; x < NI; ++x) fa[kk][x] = TA::operand(lds, wi + 32 * x, kk, lane);
-      fb[kk] = TB::operand(lds + TA::kChunks, wj, kk, lane);
-    }
+      for (int x = 0; x < 2; ++x) {
+        fa[q][x] = TA::operand(lds, wi + 32 * x, 2 * behind + q, lane);
+        fb[q][x] = TB::operand(lds + TA::kChunks, wj + 32 * x, 2 * behind + q, lane);
+      }
   };
   auto multiply = [&]() __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
+    for (int q = 0; q < 2; ++q)
 #pragma unroll
-      for (int x = 0; x < NI; ++x) mma<T>(fa[kk][x], fb[kk], acc[x][0]);
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) mma<T>(fa[q][x], fb[q][y], acc[x][y]);
     __builtin_amdgcn_s_setprio(0);
   };
   typename TB::Regs rb[2];
@@ -985,8 +990,28 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
     wait_copies<0>();
   }
   __syncthreads();
-  V* const in = wave < 2 ? lds0 : wave < 4 ? lds1 : wave < 6 ? lds2 : lds3;
-  finish<T, NI, 1>(g, p.part, acc, reinterpret_cast<float*>(in) + (wave & 1) * kStrip, lane, i0 + wi, j0 + wj);
+  // Of its 64 rows a wave of the first half of k keeps the upper 32, one of the
+  // second the lower; it adds what the other wave has of them.
+  f32x16 sum[1][2];
+  float* const given = reinterpret_cast<float*>(wave < 4 ? lds0 : lds1) + (wave & 3) * kGiven + lane;
+  const float* const got = reinterpret_cast<float*>(wave < 4 ? lds1 : lds0) + (wave & 3) * kGiven + lane;
+#pragma unroll
+  for (int y = 0; y < 2; ++y)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      given[(16 * y + r) * 64] = behind ? acc[0][y][r] : acc[1][y][r];
+      sum[0][y][r] = behind ? acc[1][y][r] : acc[0][y][r];
+    }
+  __syncthreads();
+#pragma unroll
+  for (int y = 0; y < 2; ++y)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum[0][y][r] += got[(16 * y + r) * 64];
+  __syncthreads();
+  // strips: three in each of two buffers, two in another
+  V* const in = wave < 3 ? lds0 : wave < 6 ? lds1 : lds2;
+  finish<T, 1, 2>(g, p.part, sum, reinterpret_cast<float*>(in) + wave % 3 * kStrip, lane, i0 + wi + 32 * behind,
+                  j0 + wj);
 }
 
 // The epilogue of a product whose k was split: the parts' sum (always in the
