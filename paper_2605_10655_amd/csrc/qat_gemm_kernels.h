@@ -847,11 +847,13 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
 }
 
 // For products of too few such tiles to fill the CUs: 128 x 128 of C per
-// workgroup of eight waves in turns, A always copied, three of four buffers'
-// copies under way.  A wave takes 64 x 64 of C and half of each step's k, and
-// the halves' sums meet in LDS at the end: with 64 x 32 and all of k the operands'
-// reads took 768 cycles of LDS a step, the matrix instructions 512.  bf16, 2048
-// tokens, 8192 -> 2048: XX us, 940 TFLOP/s.
+// workgroup of eight waves, A always copied, three of four buffers' copies under
+// way.  A wave takes 64 x 64 of C, four of them the even steps of k, four the
+// odd: in each turn one four read the next step's operands from LDS while the
+// others multiply the last one's, and the two sums meet in LDS at the end.
+// (With 64 x 32 and every step for each wave the operands' reads took 768 cycles
+// of LDS a step, the matrix instructions 512: 74 us; with half of each step's k
+// 69.)  bf16, 2048 tokens, 8192 -> 2048: 69 us, 1.0 PFLOP/s; fp32 2048 cubed 132.
 template <class T, int AM, int BM>
 __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int tj) {
   constexpr int kThreads = 512, BT = 128;
@@ -870,7 +872,7 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
   const int64_t i0 = (int64_t)p.i * BT, j0 = (int64_t)p.j * BT;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wi = (wave >> 1 & 1) * 64, wj = (wave & 1) * 64;
-  const bool behind = wave >= 4;   // of the later half of k, too
+  const bool odd = __builtin_amdgcn_readfirstlane(wave) >= 4;   // takes the odd steps
   f32x16 acc[2][2];
 #pragma unroll
   for (int x = 0; x < 2; ++x)
@@ -883,24 +885,24 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
   const int64_t all = g.K / TA::kStep;
   const int64_t first = all * p.part / g.splits;
   const int steps = (int)(all * (p.part + 1) / g.splits - first);
-  V fa[2][2], fb[2][2];
+  V fa[4][2], fb[4][2];
   auto read = [&](const V* lds) __attribute__((always_inline)) {
 #pragma unroll
-    for (int q = 0; q < 2; ++q)
+    for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        fa[q][x] = TA::operand(lds, wi + 32 * x, 2 * behind + q, lane);
-        fb[q][x] = TB::operand(lds + TA::kChunks, wj + 32 * x, 2 * behind + q, lane);
+        fa[kk][x] = TA::operand(lds, wi + 32 * x, kk, lane);
+        fb[kk][x] = TB::operand(lds + TA::kChunks, wj + 32 * x, kk, lane);
       }
   };
   auto multiply = [&]() __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int q = 0; q < 2; ++q)
+    for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int y = 0; y < 2; ++y) mma<T>(fa[q][x], fb[q][y], acc[x][y]);
+        for (int y = 0; y < 2; ++y) mma<T>(fa[kk][x], fb[kk][y], acc[x][y]);
     __builtin_amdgcn_s_setprio(0);
   };
   typename TB::Regs rb[2];
@@ -915,8 +917,10 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
     }
     wait_copies<0>();
     lds_barrier();
-    read(lds0);
-    multiply();
+    if (!odd) {
+      read(lds0);
+      multiply();
+    }
     lds_barrier();
   }
   if (steps > 0) {
@@ -951,18 +955,30 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
       if constexpr (!kCopyB) TB::put(rb[slot], lds + TA::kChunks, tid);
     };
     constexpr int kD = TA::kPer + (kCopyB ? TB::kPer : 0), kF = kCopyB ? 0 : TB::kLoads;
-    // Step s from `now`; `last` (read by every wave in step s - 1) receives step
-    // s + 3's copies, `then` (in step s - 2) step s + 2's codes.  Two steps'
-    // copies and codes may be under way when the next step's have landed.
-    auto step = [&](int s, int slot, V* now, V* then, V* last) __attribute__((always_inline)) {
-      read(now);
-      copy(s + 3, last);
+    // What every wave does in turn t: step t + 3's copies go to the buffer read
+    // in turn t - 1, step t + 2's codes to that of turn t - 2.  Two steps' copies
+    // and codes may be under way when those of turn t + 1 have landed.
+    auto feed = [&](int t, int slot, V* then, V* last) __attribute__((always_inline)) {
+      copy(t + 3, last);
       put(slot, then);
-      fetch(s + 4, slot);
+      fetch(t + 4, slot);
+    };
+    auto end = [&]() __attribute__((always_inline)) {
       wait_copies<2 * kD + 2 * kF>();
       lds_barrier();
+    };
+    auto read_turn = [&](int t, int slot, V* now, V* then, V* last) __attribute__((always_inline)) {
+      feed(t, slot, then, last);
+      read(now);
+      end();
+    };
+    auto multiply_turn = [&](int t, int slot, V* then, V* last) __attribute__((always_inline)) {
+      // (of 16 bits the instructions are soon done: with the copies started
+      // before them 71 us, after them 69; in fp32 the reverse, 132 and 137)
+      if (sizeof(T) == 4) feed(t, slot, then, last);
       multiply();
-      lds_barrier();
+      if (sizeof(T) == 2) feed(t, slot, then, last);
+      end();
     };
     fetch(0, 0);
     fetch(1, 1);
@@ -973,25 +989,38 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
     copy(2, lds2);
     fetch(2, 0);
     fetch(3, 1);
-    wait_copies<2 * kD + 2 * kF>();
-    lds_barrier();
-    if (behind) lds_barrier();
+    end();
+    // turns 0 .. steps, one barrier each; what is read in turn `steps` is not used
+    if (!odd) {
 #pragma unroll 1
-    for (int s = 0; s < steps; s += 4) {
-      step(s, 0, lds0, lds2, lds3);
-      if (s + 1 == steps) break;
-      step(s + 1, 1, lds1, lds3, lds0);
-      if (s + 2 == steps) break;
-      step(s + 2, 0, lds2, lds0, lds1);
-      if (s + 3 == steps) break;
-      step(s + 3, 1, lds3, lds1, lds2);
+      for (int t = 0; t <= steps; t += 4) {
+        read_turn(t, 0, lds0, lds2, lds3);
+        if (t + 1 > steps) break;
+        multiply_turn(t + 1, 1, lds3, lds0);
+        if (t + 2 > steps) break;
+        read_turn(t + 2, 0, lds2, lds0, lds1);
+        if (t + 3 > steps) break;
+        multiply_turn(t + 3, 1, lds1, lds2);
+      }
+    } else {
+      feed(0, 0, lds2, lds3);
+      end();
+#pragma unroll 1
+      for (int t = 1; t <= steps; t += 4) {
+        read_turn(t, 1, lds1, lds3, lds0);
+        if (t + 1 > steps) break;
+        multiply_turn(t + 1, 0, lds0, lds1);
+        if (t + 2 > steps) break;
+        read_turn(t + 2, 1, lds3, lds1, lds2);
+        if (t + 3 > steps) break;
+        multiply_turn(t + 3, 0, lds2, lds3);
+      }
     }
-    if (!behind) lds_barrier();
     wait_copies<0>();
   }
   __syncthreads();
-  // Of its 64 rows a wave of the first half of k keeps the upper 32, one of the
-  // second the lower; it adds what the other wave has of them.
+  // Of its 64 rows a wave of the even steps keeps the upper 32, one of the odd
+  // the lower; it adds what the other wave has of them.
   f32x16 sum[1][2];
   float* const given = reinterpret_cast<float*>(wave < 4 ? lds0 : lds1) + (wave & 3) * kGiven + lane;
   const float* const got = reinterpret_cast<float*>(wave < 4 ? lds1 : lds0) + (wave & 3) * kGiven + lane;
@@ -999,8 +1028,8 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
   for (int y = 0; y < 2; ++y)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      given[(16 * y + r) * 64] = behind ? acc[0][y][r] : acc[1][y][r];
-      sum[0][y][r] = behind ? acc[1][y][r] : acc[0][y][r];
+      given[(16 * y + r) * 64] = odd ? acc[0][y][r] : acc[1][y][r];
+      sum[0][y][r] = odd ? acc[1][y][r] : acc[0][y][r];
     }
   __syncthreads();
 #pragma unroll
@@ -1010,7 +1039,7 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
   __syncthreads();
   // strips: three in each of two buffers, two in another
   V* const in = wave < 3 ? lds0 : wave < 6 ? lds1 : lds2;
-  finish<T, 1, 2>(g, p.part, sum, reinterpret_cast<float*>(in) + wave % 3 * kStrip, lane, i0 + wi + 32 * behind,
+  finish<T, 1, 2>(g, p.part, sum, reinterpret_cast<float*>(in) + wave % 3 * kStrip, lane, i0 + wi + 32 * odd,
                   j0 + wj);
 }
 

@@ -45,8 +45,8 @@ inline GemmPlan gemm_plan(int dtype, int64_t I, int64_t J, int64_t K) {
     double step, fixed;
     int at_once;
   };
-  static constexpr Kind half[] = {{256, 2400, 9000, 256}, {128, 750, 4000, 256}, {64, 480, 3000, 512}};
-  static constexpr Kind full[] = {{256, 8600, 12000, 256}, {128, 2300, 5000, 256}, {64, 1150, 3500, 512}, {64, 700, 3500, 256}};
+  static constexpr Kind half[] = {{256, 2400, 9000, 256}, {128, 700, 4000, 256}, {64, 480, 3000, 512}};
+  static constexpr Kind full[] = {{256, 8250, 12000, 256}, {128, 2150, 5000, 256}, {64, 1150, 3500, 512}, {64, 700, 3500, 256}};
   const int64_t steps = ceil_div(K, dtype == kF32 ? 32 : 64);
   GemmPlan best = {};
   double least = 0.;
