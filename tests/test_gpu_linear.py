@@ -695,6 +695,90 @@ def test_no_gradient_keeps_no_checkpoint(monkeypatch):
         linear_act8(x, W, b, r, "gelu")
 
 
+def test_offsets_past_32_bits():
+    """70000 x 32768: every operator's last rows, which lie past 2^31 values."""
+    M, N, K, last = 70000, 32768, 64, 32
+    r0 = M - M % 32                                   # a group of 16 rows ends it
+    g = torch.Generator().manual_seed(2)
+    x, W = torch.randn(M, K, generator=g).bfloat16(), (0.1 * torch.randn(N, K, generator=g)).bfloat16()
+    xd, Wd = x.cuda(), W.cuda()
+    y, z8 = Q.linear_act(xd, Wd, None, None, "silu", save=True)
+    want, bound, z, zb = R.linear64(x[-last:], W, None, None, "silu", torch.bfloat16)
+    within(y[-last:], want, bound, "y")
+    step = z8.scales[-1].cpu().double().abs()
+    off = (Q.act8_load(z8, torch.float32)[r0:].cpu().double() - z[r0 - M:]).abs()
+    assert bool((off <= 0.5 * step + zb[r0 - M:] * (1 + 1e-6)).all())
+    del y
+    # an activation of that size
+    dy = torch.zeros(M, N, dtype=torch.bfloat16, device="cuda")
+    tail = torch.randn(last, N, generator=g).bfloat16()
+    dy[-last:] = tail.cuda()
+    a = Q.act8_store(dy)
+    assert torch.equal(a.codes[-1], Q.act8_store(dy[r0:]).codes[0]) and not a.codes[:100].any()
+    assert torch.equal(Q.act8_load(a)[r0:], Q.act8_load(Q.act8_store(dy[r0:])))
+    del a
+    # and the backward pass: all rows but the last give zeros
+    x8 = Q.act8_store(xd)
+    dx, dW, db = Q.linear_act_vjp(dy, x8, Wd, z8, "silu")
+    xv = Q.act8_load(x8)[-last:].cpu().double()
+    zv = Q.act8_load(z8, torch.float32)[-last:].cpu().double()
+    ref = R.vjp64(tail, xv, W, zv, "silu", torch.bfloat16)
+    # the sums have M terms, all but the last zero: no further rounding
+    for got, r, b, what in ((dx[-last:], *ref[:2], "dx"), (dW, *ref[2:4], "dW"), (db, *ref[4:], "dbias")):
+        within(got, r, b, what)
+    assert not dx[:-last].any()
+
+
+@pytest.mark.parametrize("n,k,V,N,K", [(16, 2, 1, 2048, 1024), (16, 4, 2, 1100, 1024)])
+def test_captured_codes_replay(n, k, V, N, K):
+    """The kernels whose tables take most of the LDS, captured."""
+    W, s, packed, cd, sd = _coded(4, N, K, n, k, V, 256)
+    xs = [torch.randn(M, K, device="cuda", dtype=torch.bfloat16) for M in (1, 16, 40, 100)]
+
+    def step():
+        return [Q.trellis_linear(x, packed, cd, n, k, V, scales=sd) for x in xs]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(3):
+        for x in xs:
+            x.normal_()
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), i
+
+
+def test_documented_forms():
+    """Three dimensions with outputs given, shapes of codebook and scales that
+    mean the same, a checkpoint read in another type."""
+    g = torch.Generator().manual_seed(6)
+    x, W = torch.randn(2, 9, 48, generator=g).cuda(), torch.randn(20, 48, generator=g).cuda()
+    r = torch.randn(2, 9, 20, generator=g).cuda()
+    out = torch.empty(2, 9, 20, device="cuda")
+    y = Q.linear_act(x, W, None, r, "gelu", out=out)
+    assert y is out and torch.equal(y.view(18, 20), Q.linear_act(x.view(18, 48), W, None, r.view(18, 20), "gelu"))
+    dx, dW, _ = Q.linear_act_vjp(r, Q.act8_store(x), W)
+    assert dx.shape == x.shape and torch.equal(dW, Q.linear_act_vjp(r.view(18, 20), Q.act8_store(x), W)[1])
+    W, s, packed, cd, sd = _coded(5, 12, 64, 8, 2, 1, 32)
+    want = Q.trellis_linear(x[..., :64 - 16].new_ones(3, 64), packed, cd, 8, 2, 1, 32, scales=sd)
+    out = torch.empty(3, 12, device="cuda")
+    got = Q.trellis_linear(torch.ones(3, 64, device="cuda"), packed.view(-1, packed.shape[-1]), cd.view(256, 1), 8, 2, 1,
+                           32, scales=sd.reshape(-1), out=out)
+    assert got is out and torch.equal(got, want)
+    a = Q.act8_store(torch.randn(40, 6, generator=g).cuda())
+    v = Q.act8_load(a)
+    for t in (torch.float16, torch.bfloat16):
+        assert torch.equal(Q.act8_load(a, t), v.to(t))
+
+
 def test_same_tensors_twice_and_views():
     """One tensor as several operands, overlapping views as inputs, and a
     batch whose padding rows hold NaN."""
