@@ -526,9 +526,9 @@ __device__ __forceinline__ void finish(const GemmArgs& g, int part, f32x16 (&acc
 // under way (codes always so, becoming T on the way).  No step has a branch:
 // what is left of k beyond whole steps goes first, and steps past the last
 // fetch that one again, into buffers that nothing reads any more.  Tiles of 64
-// are bound by a step's latency (LDS reads, a barrier) beside few matrix
-// instructions: fp32, 500 tokens, 1024 -> 2048: 26 us, half of the matrix
-// instructions' rate; fp16 through registers, 333 tokens, 777 -> 1000: 12.5 us.
+// are bound by the matrix instructions in fp32 (500 tokens, 1024 -> 2048: 25
+// us; eight waves in turns, as below, take as long) and by a step's latency in
+// 16 bits (fp16 through registers, 333 tokens, 777 -> 1000: 12 us).
 template <class T, int AM, int BM, int BT, bool COPY>
 __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
   constexpr int kThreads = 256, W = BT / 2, NT = W / 32;
