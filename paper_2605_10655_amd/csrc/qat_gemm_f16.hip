@@ -8,9 +8,9 @@
 namespace bcjr {
 namespace qlin {
 
-template int gemm<f16, kRow, kRow>(GemmArgs, void*, hipStream_t, bool);
-template int gemm<f16, kRow, kCol>(GemmArgs, void*, hipStream_t, bool);
-template int gemm<f16, kCol, kCodes>(GemmArgs, void*, hipStream_t, bool);
+template int gemm<f16, kRow, kRow>(GemmArgs, void*, hipStream_t, bool, bool);
+template int gemm<f16, kRow, kCol>(GemmArgs, void*, hipStream_t, bool, bool);
+template int gemm<f16, kCol, kCodes>(GemmArgs, void*, hipStream_t, bool, bool);
 template int gemm_large<f16, kCol, kCol>(GemmArgs, const GemmPlan&, void*, hipStream_t);
 
 }  // namespace qlin

@@ -8,9 +8,9 @@
 namespace bcjr {
 namespace qlin {
 
-template int gemm<float, kRow, kRow>(GemmArgs, void*, hipStream_t, bool);
-template int gemm<float, kRow, kCol>(GemmArgs, void*, hipStream_t, bool);
-template int gemm<float, kCol, kCodes>(GemmArgs, void*, hipStream_t, bool);
+template int gemm<float, kRow, kRow>(GemmArgs, void*, hipStream_t, bool, bool);
+template int gemm<float, kRow, kCol>(GemmArgs, void*, hipStream_t, bool, bool);
+template int gemm<float, kCol, kCodes>(GemmArgs, void*, hipStream_t, bool, bool);
 template int gemm_large<float, kCol, kCol>(GemmArgs, const GemmPlan&, void*, hipStream_t);
 
 }  // namespace qlin

@@ -95,8 +95,8 @@ struct Tile {
 
   // Asynchronous copy of k0 .. k0 + kStep - 1 into LDS, straight from memory:
   // needs p and ld aligned to 16 bytes, K (row) or R (col) a whole number of
-  // chunks (or the last row's memory to go on to one), and a tile's span below
-  // 2 GiB.  A wave's 64 chunks go to 64
+  // chunks (or rows that go on to one, by rows with zeros), and a tile's span
+  // below 2 GiB.  A wave's 64 chunks go to 64
   // consecutive places, so each lane fetches the chunk that belongs at its
   // place: byte offsets from the tile's start, the same in every step.  Rows
   // past the end read the last one's (their sums are not stored), k past the

@@ -78,11 +78,12 @@ void launch_gemm(const GemmArgs& g, const GemmPlan& p, hipStream_t stream) {
 }
 
 // Whether tiles of an operand can be copied straight into LDS (Tile::copy).
-// padded: memory goes on to the end of the last row's leading dimension.
+// padded: rows go on to a whole number of 16 bytes, in an operand by rows with
+// zeros (as its k is then multiplied).
 inline bool copies(int mode, const void* p, int64_t ld, int64_t rows, int64_t K, int es, int tile, bool padded) {
   if (mode == kCodes) return true;
   const int e = 16 / es;
-  return !misaligned(p, 16) && ld % e == 0 && (mode == kRow ? K % e == 0 : padded || rows % e == 0) &&
+  return !misaligned(p, 16) && ld % e == 0 && (padded || (mode == kRow ? K : rows) % e == 0) &&
          (int64_t)(mode == kRow ? tile : 8 * e) * ld * es < ((int64_t)1 << 31);
 }
 
@@ -108,10 +109,10 @@ int gemm_large(GemmArgs g, const GemmPlan& p, void* ws, hipStream_t stream) {
   return p.splits > 1 ? join<T>(g, stream) : BCJR_OK;
 }
 
-// The product and its epilogue (of zero sums where K == 0).  a_padded: as
-// padded of copies(), for A.
+// The product and its epilogue (of zero sums where K == 0).  a_padded, b_padded:
+// as padded of copies().
 template <class T, int AM, int BM>
-int gemm(GemmArgs g, void* ws, hipStream_t stream, bool a_padded = false) {
+int gemm(GemmArgs g, void* ws, hipStream_t stream, bool a_padded = false, bool b_padded = false) {
   if (g.I == 0 || g.J == 0) return BCJR_OK;
   constexpr int es = (int)sizeof(T), dtype = es == 4 ? kF32 : kBF16;
   GemmPlan p = gemm_plan(dtype, g.I, g.J, g.K);
@@ -119,7 +120,7 @@ int gemm(GemmArgs g, void* ws, hipStream_t stream, bool a_padded = false) {
   if (!grid_fits((int64_t)p.ti * p.tj * p.splits, p.tile == 256 ? 2048 : p.tile == 128 ? 512 : 256))
     return BCJR_ERR_UNSUPPORTED;
   const bool copied = copies(AM, g.a, g.lda, g.I, g.K, es, p.tile, a_padded) &&
-                      copies(BM, g.b, g.ldb, g.J, g.K, es, p.tile, false);
+                      copies(BM, g.b, g.ldb, g.J, g.K, es, p.tile, b_padded);
   if constexpr (BM != kCodes)
     if (copied && p.tile == 256) return gemm_large<T, AM, BM>(g, p, ws, stream);
   if (p.tile == 256) {

@@ -16,9 +16,9 @@ namespace bcjr {
 namespace qlin {
 
 #define QAT_GEMM_EXTERN(T)                                                   \
-  extern template int gemm<T, kRow, kRow>(GemmArgs, void*, hipStream_t, bool);     \
-  extern template int gemm<T, kRow, kCol>(GemmArgs, void*, hipStream_t, bool);     \
-  extern template int gemm<T, kCol, kCodes>(GemmArgs, void*, hipStream_t, bool);   \
+  extern template int gemm<T, kRow, kRow>(GemmArgs, void*, hipStream_t, bool, bool);   \
+  extern template int gemm<T, kRow, kCol>(GemmArgs, void*, hipStream_t, bool, bool);   \
+  extern template int gemm<T, kCol, kCodes>(GemmArgs, void*, hipStream_t, bool, bool); \
   extern template int gemm_large<T, kCol, kCol>(GemmArgs, const GemmPlan&, void*, hipStream_t);
 QAT_GEMM_EXTERN(bf16)
 QAT_GEMM_EXTERN(f16)
@@ -62,8 +62,63 @@ bool bands_fit(int dtype, int64_t rows, int64_t cols) {
   return grid_fits(ceil_div(rows, kRows) * ceil_div(cols, wide), kGroupThreads);
 }
 
-int run_linear(const GemmArgs& g, int dtype, void* ws, hipStream_t stream) {
-  return by_type(dtype, [&](auto t) -> int { return gemm<decltype(t), kRow, kRow>(g, ws, stream); });
+// n rounded up to whole 16 bytes
+int64_t whole(int dtype, int64_t n) {
+  const int e = 16 / elem_size(dtype);
+  return ceil_div(n, e) * e;
+}
+
+// Whether operands of a product I x J whose rows of n values make no whole 16
+// bytes (along k, or b's columns) are padded first: where tiles are large, each
+// value padded is used often and a launch of 4 us is little (bf16, us, padded and through registers: 8191 x 6282, K = 1023 147 and
+// 389, 4096 x 4097, K = 4099 227 and 322, 3666 x 224, K = 4685 43 and 42; fp32:
+// 888 and 1024, 1186 and 1184, 108 and 95; bf16 1000 x 777, K = 999 14.0 and 13.1).
+bool pads(const GemmPlan& p, int dtype, int64_t I, int64_t J, int64_t K, int64_t n) {
+  return p.tile >= 128 && I >= 512 && J >= 512 && (double)I * J * K >= 2147483648. && whole(dtype, n) != n;
+}
+
+template <class T>
+int pad(const void* a, int64_t lda, int64_t rows, int64_t cols, void* to, const void* b, int64_t ldb, int64_t brows,
+        void* bto, hipStream_t stream) {
+  const int64_t chunks = ceil_div(cols, kPer16<T>);
+  const int64_t first = ceil_div(rows * chunks, 256), all = first + (b ? ceil_div(brows * chunks, 256) : 0);
+  if (!grid_fits(all, 256)) return BCJR_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL(pad_kernel<T>, dim3((unsigned)all), dim3(256), 0, stream, Pad{a, lda, to, rows, cols, chunks},
+                     Pad{b, ldb, bto, brows, cols, chunks}, (unsigned)first);
+  return launched();
+}
+
+struct LinearPlan {
+  size_t part, x, W, total;
+};
+
+// the partial sums, then x and W padded
+LinearPlan linear_plan(int dtype, int64_t M, int64_t N, int64_t K) {
+  LinearPlan p = {};
+  const GemmPlan g = gemm_plan(dtype, M, N, K);
+  p.part = g.part;
+  if (pads(g, dtype, M, N, K, K)) {
+    p.x = align_up((size_t)(M * whole(dtype, K)) * elem_size(dtype));
+    p.W = align_up((size_t)(N * whole(dtype, K)) * elem_size(dtype));
+  }
+  p.total = p.part + p.x + p.W;
+  return p;
+}
+
+int run_linear(GemmArgs g, int dtype, char* ws, hipStream_t stream) {
+  return by_type(dtype, [&](auto t) -> int {
+    using T = decltype(t);
+    const LinearPlan p = linear_plan(dtype, g.I, g.J, g.K);
+    if (p.x) {
+      char *x = ws + p.part, *W = x + p.x;
+      const int st = pad<T>(g.a, g.lda, g.I, g.K, x, g.b, g.ldb, g.J, W, stream);
+      if (st != BCJR_OK) return st;
+      g.a = x;
+      g.b = W;
+      g.lda = g.ldb = whole(dtype, g.K);
+    }
+    return gemm<T, kRow, kRow>(g, ws, stream, p.x != 0, p.x != 0);
+  });
 }
 
 FewArgs few_args(const void* x, int64_t ldx, const void* bias, const void* residual, int64_t ldr, void* y,
@@ -116,13 +171,13 @@ int run_small_vjp(SmallVjp a, hipStream_t stream) {
 }
 
 struct VjpPlan {
-  size_t dz, part, x, sums, total;
+  size_t dz, part, x, W, sums, total;
   int64_t ldz, ldx;
   GemmPlan dW;
 };
 
-// dz, the groups' sums of dbias, x for a large dW, then the partial sums of the
-// products.  Workgroups that turn x's codes into T for themselves do it N / 256
+// dz (or dy padded), the groups' sums of dbias, x for a large dW, W padded for
+// dx, then the partial sums of the products.  Workgroups that turn x's codes into T for themselves do it N / 256
 // times over: from tiles of 256 on x is read back once instead (4096 tokens,
 // 2048 x 8192, bf16: 174 us against 121 + 21; with tiles of 128 that costs as
 // much as it gives, 44.7 and 44.3 us for 2048 cubed, with smaller ones 5 us
@@ -130,16 +185,17 @@ struct VjpPlan {
 VjpPlan vjp_plan(int dtype, int64_t M, int64_t N, int64_t K, int act) {
   VjpPlan p = {};
   if (small_vjp(M, N, K)) return p;
-  const int es = elem_size(dtype), e = 16 / es;
-  p.ldz = ceil_div(N, e) * e;
-  p.ldx = ceil_div(K, e) * e;
-  p.dz = act == kActNone ? 0 : align_up((size_t)(M * p.ldz) * es);
+  const int es = elem_size(dtype);
+  const GemmPlan dx = M ? gemm_plan(dtype, M, K, N) : GemmPlan{};
+  p.ldz = whole(dtype, N);
+  p.ldx = whole(dtype, K);
+  p.dz = act == kActNone && !pads(dx, dtype, M, K, N, N) ? 0 : align_up((size_t)(M * p.ldz) * es);
+  p.W = pads(dx, dtype, M, K, N, K) ? align_up((size_t)(N * p.ldx) * es) : 0;
   p.part = align_up((size_t)(2 * ceil_div(M, kRows) * N) * sizeof(float));
   p.dW = gemm_plan(dtype, N, K, M);
   p.x = p.dW.tile == 256 ? align_up((size_t)(M * p.ldx) * es) : 0;
-  const size_t dx = M ? gemm_plan(dtype, M, K, N).part : 0;
-  p.sums = dx > p.dW.part ? dx : p.dW.part;
-  p.total = p.dz + p.part + p.x + p.sums;
+  p.sums = dx.part > p.dW.part ? dx.part : p.dW.part;
+  p.total = p.dz + p.part + p.x + p.W + p.sums;
   return p;
 }
 
@@ -236,7 +292,7 @@ int qat_act8_load(const int8_t* codes, const uint16_t* scales, int64_t rows, int
 
 size_t qat_linear_act_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K) {
   if (!dtype_ok(dtype) || !dims_ok(M, N, K) || !dims_fit(M, N, K) || M == 0) return 0;
-  return gemm_plan(dtype, M, N, K).part;
+  return linear_plan(dtype, M, N, K).total;
 }
 
 int qat_linear_act(const void* x, int64_t ldx, const void* W, int64_t ldw, const void* bias, const void* residual,
@@ -256,7 +312,7 @@ int qat_linear_act(const void* x, int64_t ldx, const void* W, int64_t ldw, const
   if (M <= 16 && !z_codes)
     return run_few(few_args(x, ldx, bias, residual, ldr, y, ldy, activation, M, N, K), W, ldw, dtype, stream);
   const GemmArgs g = {x, W, ldx, ldw, nullptr, M, N, K, bias, residual, ldr, y, ldy, z_codes, z_scales, activation};
-  return run_linear(g, dtype, workspace, stream);
+  return run_linear(g, dtype, static_cast<char*>(workspace), stream);
 }
 
 size_t qat_linear_act_vjp_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K, int activation) {
@@ -289,7 +345,7 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
   return by_type(dtype, [&](auto t) -> int {
     using T = decltype(t);
     char* ws = static_cast<char*>(workspace);
-    void* sums = ws + p.dz + p.part + p.x;
+    void* sums = ws + p.dz + p.part + p.x + p.W;
     const T* dz = static_cast<const T*>(dy);
     int64_t ldz = ldd;
     float* part = reinterpret_cast<float*>(ws + p.dz);
@@ -307,19 +363,32 @@ int qat_linear_act_vjp(const void* dy, int64_t ldd, const int8_t* x_codes, const
         ldz = p.ldz;
       }
     }
+    if (p.dz && activation == kActNone && M > 0 && (dx || dW)) {
+      const int st = pad<T>(dy, ldd, M, N, ws, nullptr, 0, 0, nullptr, stream);
+      if (st != BCJR_OK) return st;
+      dz = reinterpret_cast<const T*>(ws);
+      ldz = p.ldz;
+    }
     if (dbias) {
       hipLaunchKernelGGL(dbias_kernel<T>, dim3((unsigned)ceil_div(N, 64)), dim3(1024), 0, stream, (const float*)part,
                          ceil_div(M, kRows), N, static_cast<T*>(dbias));
       if (launched() != BCJR_OK) return BCJR_ERR_HIP;
     }
     if (dx && M > 0) {
-      const GemmArgs g = {dz, W, ldz, ldw, nullptr, M, K, N, nullptr, nullptr, 0, dx, K, nullptr, nullptr, kActNone};
-      const int st = gemm<T, kRow, kCol>(g, sums, stream);
+      GemmArgs g = {dz, W, ldz, ldw, nullptr, M, K, N, nullptr, nullptr, 0, dx, K, nullptr, nullptr, kActNone};
+      if (p.W) {
+        void* to = ws + p.dz + p.part + p.x;
+        const int st = pad<T>(W, ldw, N, K, to, nullptr, 0, 0, nullptr, stream);
+        if (st != BCJR_OK) return st;
+        g.b = to;
+        g.ldb = p.ldx;
+      }
+      const int st = gemm<T, kRow, kCol>(g, sums, stream, p.dz != 0, p.W != 0);
       if (st != BCJR_OK) return st;
     }
     if (dW) {
       GemmArgs g = {dz, x_codes, ldz, 0, x_scales, N, K, M, nullptr, nullptr, 0, dW, K, nullptr, nullptr, kActNone};
-      const bool padded = activation != kActNone;
+      const bool padded = p.dz != 0;
       if (!p.x || !bands_fit(dtype, M, K) || !copies(kCol, dz, ldz, N, M, (int)es, 256, padded))
         return gemm<T, kCol, kCodes>(g, sums, stream, padded);
       T* x = reinterpret_cast<T*>(ws + p.dz + p.part);

@@ -187,9 +187,15 @@ __global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__
   constexpr int C = kCols<T>, kHalf = kRows / 2;
   const int h = blockIdx.x & 1;
   const Band b = band_of<C>(cols, blockIdx.x >> 1);
-  if (b.n == 0) return;
   const int64_t at = b.g * cols + b.c, r0 = b.g * kRows + kHalf * h;
   const int left = (int)(rows - r0 < kHalf ? rows - r0 : kHalf);   // 0 or less: none
+  if (b.n == 0) {
+    // zeros to the end of dz's rows (ldz is a multiple of C)
+    const float zeros[C] = {};
+    if (ACT != kActNone && b.c < ldz)
+      for (int i = 0; i < left; ++i) set<T, C>(dz + (r0 + i) * ldz + b.c, C, zeros);
+    return;
+  }
   float eights[2][C] = {};   // sums of eight rows
   if (left > 0) {
     u32x4 w[C];
@@ -211,7 +217,11 @@ __global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__
         for (int c = 0; c < C; ++c) v[i][c] = scaled(act_slope(q8_value(code_at(&w[c], i), s[c]), ACT), v[i][c]);
       }
       if (i < left) {
-        if (ACT != kActNone) set<T, C>(dst + i * ldz, b.n, v[i]);
+        if (ACT != kActNone) {
+#pragma unroll
+          for (int c = 0; c < C; ++c) v[i][c] = c < b.n ? v[i][c] : 0.f;
+          set<T, C>(dst + i * ldz, C, v[i]);
+        }
 #pragma unroll
         for (int c = 0; c < C; ++c) eights[i / 8][c] += v[i][c];
       }
@@ -221,6 +231,38 @@ __global__ __launch_bounds__(kGroupThreads) void dz_kernel(const T* __restrict__
 #pragma unroll
     for (int c = 0; c < C; ++c)
       if (c < b.n) part[(2 * b.g + h) * cols + b.c + c] = eights[0][c] + eights[1][c];
+}
+
+// Up to two matrices into rows of whole 16 bytes, zeros behind their columns: a
+// thread per 16 bytes written.  Bound by its bytes; the rule for it stands with
+// its call.
+struct Pad {
+  const void* src;
+  int64_t ld;
+  void* dst;
+  int64_t rows, cols, chunks;   // chunks: of a row written
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void pad_kernel(Pad a, Pad b, unsigned first) {
+  using V = typename Vec<T>::type;
+  constexpr int E = kPer16<T>;
+  const Pad p = blockIdx.x < first ? a : b;
+  const int64_t id = (int64_t)(blockIdx.x - (blockIdx.x < first ? 0 : first)) * 256 + threadIdx.x;
+  if (id >= p.rows * p.chunks) return;
+  const int64_t row = id / p.chunks, c = (id - row * p.chunks) * E, n = p.cols - c;
+  const T* src = static_cast<const T*>(p.src) + row * p.ld + c;
+  V v;
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = (T)0.f;
+  if (n >= E) {
+    __builtin_memcpy(&v, src, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (e < n) v[e] = src[e];
+  }
+  static_cast<V*>(p.dst)[id] = v;
 }
 
 // The groups' sums of a column, in 64 bits and a fixed order: 16 threads take

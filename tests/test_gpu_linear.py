@@ -256,6 +256,24 @@ def test_vjp_at_the_bounds_of_its_small_form(t, M, N, K):
 
 
 @pytest.mark.parametrize("t", R.TYPES)
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("M,N,K,pad", [(1500, 1501, 1003, 0), (2049, 2051, 517, 3), (1800, 1600, 777, 0), (1800, 777, 1600, 5),
+                                       (4097, 515, 1030, 1)])
+def test_large_odd_sizes(t, act, M, N, K, pad):
+    """Rows of no whole 16 bytes are padded before large products, in both
+    directions, with and without dz; what lies behind them does not count."""
+    dt = R.TYPES[t]
+    _say(f"[odd] {t} {act} {M}x{N}x{K} pad {pad}")
+    host, devi = _layer(M, M, N, K, dt, pad)
+    y, yb, z, zb = R.linear64(*host, act, dt)
+    got, z8 = Q.linear_act(*devi, act, save=True)
+    within(got, y, yb, "y")
+    ref, call = _vjp_case(M + N, M, N, K, dt, act, pad, dense=act != "none")
+    for got, r, b, what in zip(Q.linear_act_vjp(*call), ref[::2], ref[1::2], ("dx", "dW", "dbias")):
+        within(got, r, b, f"{what} {t} {M}x{N}x{K}")
+
+
+@pytest.mark.parametrize("t", R.TYPES)
 @pytest.mark.parametrize("act", R.ACTS)
 @pytest.mark.parametrize("M,pad", [(1, 0), (40, 3), (150, 8), (400, 1)])
 def test_vjp_forms(t, act, M, pad):
