@@ -146,13 +146,15 @@ def _apart(name, out, *inputs):
                 raise ValueError(f"{name} overlaps an input")
 
 
-def _output(name, out, shape, dtype, device, *inputs):
+def _output(name, out, shape, x, *inputs):
+    """out, or a new tensor of x's type and device."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return x.new_empty(shape)
+    dtype, device = x.dtype, x.device
     _tensor(name, out, dtype, device)
     if tuple(out.shape) != tuple(shape) or not out.is_contiguous():
         raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}, got {tuple(out.shape)}")
-    _apart(name, out, *inputs)
+    _apart(name, out, x, *inputs)
     return out
 
 
@@ -190,7 +192,7 @@ def _on(stream, device):
     """The tensors' device as the current one for a call's launches."""
     if stream is not None and stream.device != device:
         raise ValueError(f"stream is on {stream.device}, the call's tensors on {device}")
-    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    return _HERE if torch._C._cuda_getDevice() == device.index else torch.cuda.device(device)
 
 
 def _stream(stream, device):
@@ -269,7 +271,13 @@ def act8_load(a: Act8, dtype=None, *, out=None, stream=None):
         raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
     dev = a.codes.device
     with _on(stream, dev):
-        out = _output("out", out, (a.rows, a.cols), dtype, dev, a.codes, a.scales)
+        if out is None:
+            out = torch.empty((a.rows, a.cols), dtype=dtype, device=dev)
+        else:
+            _tensor("out", out, dtype, dev)
+            if tuple(out.shape) != (a.rows, a.cols) or not out.is_contiguous():
+                raise ValueError(f"out must be contiguous with shape {(a.rows, a.cols)}, got {tuple(out.shape)}")
+            _apart("out", out, a.codes, a.scales)
         rc = lib.qat_act8_load(_ptr(a.codes), _ptr(a.scales), a.rows, a.cols, _ptr(out), DTYPES[dtype],
                                a.cols, _stream(stream, dev))
         _raise("qat_act8_load", rc)
@@ -295,7 +303,7 @@ def linear_act(x, W, bias=None, residual=None, activation="none", *, out=None, s
     _vector("bias", bias, N, t, dev)
     res, ldr = (None, 0) if residual is None else _matrix("residual", residual, t, dev, M, N)
     with _on(stream, dev):
-        y = _output("out", out, (*x.shape[:-1], N), t, dev, m, w, bias, res)
+        y = _output("out", out, (*x.shape[:-1], N), m, w, bias, res)
         z8 = _new_act8(M, N, torch.float32, dev) if save else None
         ws = _space(workspace, _linear_bytes(DTYPES[t], M, N, K), dev)
         rc = lib.qat_linear_act(_ptr(m), ldx, _ptr(w), ldw, _ptr(bias), _ptr(res), ldr, DTYPES[t], act, M,
@@ -333,9 +341,9 @@ def linear_act_vjp(dy, x8, W, z8=None, activation="none", *, want_dx=True, want_
             raise ValueError(f"activation {activation!r} needs z8")
         _check_act8("z8", z8, M, N, torch.float32, dev)
     with _on(stream, dev):
-        dx = torch.empty((*dy.shape[:-1], K), dtype=t, device=dev) if want_dx else None
-        dW = torch.empty((N, K), dtype=t, device=dev) if want_dW else None
-        db = torch.empty(N, dtype=t, device=dev) if want_dbias else None
+        dx = d.new_empty((*dy.shape[:-1], K)) if want_dx else None
+        dW = d.new_empty((N, K)) if want_dW else None
+        db = d.new_empty(N) if want_dbias else None
         ws = _space(workspace, _vjp_bytes(DTYPES[t], M, N, K, act), dev)
         rc = lib.qat_linear_act_vjp(_ptr(d), ldd, _ptr(x8.codes) if want_dW else None,
                                     _ptr(x8.scales) if want_dW else None, _ptr(w), ldw,
@@ -464,7 +472,7 @@ def trellis_linear(x, packed, codebook, state_bits: int, k: int, V: int = 1, blo
     _vector("bias", bias, N, t, dev)
     res, ldr = (None, 0) if residual is None else _matrix("residual", residual, t, dev, M, N)
     with _on(stream, dev):
-        y = _output("out", out, (*x.shape[:-1], N), t, dev, m, packed, codebook, scales, bias, res)
+        y = _output("out", out, (*x.shape[:-1], N), m, packed, codebook, scales, bias, res)
         ws = _space(workspace, _trellis_bytes(DTYPES[t], M, N, K, int(state_bits), int(k), int(V),
                                               int(block)), dev)
         rc = lib.trellis_linear(_ptr(m), ldx, _ptr(packed), _ptr(codebook), int(state_bits), int(k), int(V),
