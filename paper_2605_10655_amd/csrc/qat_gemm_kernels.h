@@ -170,7 +170,9 @@ struct Tile {
     if (MODE == kCodes) {
       // 16 codes a load, a row's runs by neighbouring threads.  Every thread
       // loads, those past the tile its first run again: the number of loads
-      // under way is then the same in every wave.
+      // under way is then the same in every wave.  A run past the end of k is
+      // zero with a scale of zero: that of another group could be negative, and
+      // put() would turn the run into NaN.
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int at = (i * THREADS + tid) % (R * kRuns);
@@ -182,7 +184,8 @@ struct Tile {
         u32x4 q = *reinterpret_cast<const u32x4*>(static_cast<const int8_t*>(p) + o * kRows + (in ? k % kRows : 0));
         if (!in) q = u32x4{0, 0, 0, 0};
         __builtin_memcpy(&g.v[i], &q, 16);
-        g.s[i] = scales[o];
+        const uint16_t sb = scales[o];
+        g.s[i] = in ? sb : (uint16_t)0;
       }
       return;
     }

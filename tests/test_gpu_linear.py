@@ -326,6 +326,27 @@ def test_vjp_of_a_non_finite_row():
     assert torch.isfinite(got[1][:5]).all() and torch.isfinite(got[2][:5]).all()
 
 
+@pytest.mark.parametrize("t", R.TYPES)
+@pytest.mark.parametrize("M,N,K", [(1000, 136, 264), (1025, 200, 96), (80, 300, 520), (1000, 1536, 1536),
+                                   (49, 2048, 2056), (1040, 1504, 1200), (1100, 4096, 4096)])
+def test_vjp_of_a_non_finite_first_value(t, M, N, K):
+    """A bad value in x's first group, whose scale is read where runs past the
+    last token are, stays in its column of dW: tiles of every size, and tokens
+    that end inside a step of each."""
+    dt = R.TYPES[t]
+    _, xd = rand(1, M, K, dtype=dt)
+    _, dyd = rand(3, M, N, dtype=dt, scale=M ** -0.5)
+    _, zd = rand(4, M, N)
+    z8 = Q.act8_store(zd)
+    clean = Q.linear_act_vjp(dyd, Q.act8_store(xd), None, z8, "silu", want_dx=False)
+    for value in (float("nan"), float("-inf")):
+        bad = xd.clone()
+        bad[0, 0] = value
+        got = Q.linear_act_vjp(dyd, Q.act8_store(bad), None, z8, "silu", want_dx=False)
+        assert torch.isnan(got[1][:, 0]).all()
+        assert torch.equal(got[1][:, 1:], clean[1][:, 1:]) and torch.equal(got[2], clean[2])
+
+
 @pytest.mark.parametrize("act", R.ACTS)
 def test_gradients_match_differences(act):
     """linear_act8's gradients in fp32 against central differences of the
