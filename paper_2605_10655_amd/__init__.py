@@ -156,18 +156,21 @@ def _check_out(name, t, shape, device, dtype=None):
 
 
 def _keep_alive(stream, *tensors):
-    """Tensors this module allocated come from PyTorch's caching allocator on
-    the current stream; when the launch went to another stream, tell the
-    allocator so that their memory is not handed out again while the
-    kernels may still use it."""
+    """A call's outputs and workspace, when its launch went to another stream
+    than the current one: the allocator is told of both, so that the memory
+    (from `stream`'s pool, or the caller's own) is not handed out again while
+    the kernels, or what the caller does with the outputs, may still use
+    it."""
     if stream is None:
         return
     torch = _torch()
-    if stream == torch.cuda.current_stream(stream.device):
+    here = torch.cuda.current_stream(stream.device)
+    if stream == here:
         return
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
+            t.record_stream(here)
 
 
 def _ws_bytes(ws):

@@ -21,8 +21,11 @@ Tensors are float32, bfloat16 or float16, the same for every operand of a
 call.  Matrices may have a row stride (columns contiguous, rows not
 overlapping); x, residual and dy may have more than two dimensions if they are
 contiguous.  Calls run on the tensors' device, on its current stream or
-`stream`; outputs and workspaces come from PyTorch's allocator, so that calls
-captured into a graph own theirs.  The autograd node is
+`stream`; outputs and workspaces come from PyTorch's allocator, from the pool
+of the stream that the call runs on, so that no two streams share a workspace
+and calls captured into a graph own theirs.  On `stream` the inputs have to be
+ready, and live until it is done; what comes back may be used on the current
+stream once that has waited for `stream`.  The autograd node is
 ``autograd.linear_act8``.
 """
 from __future__ import annotations
@@ -189,9 +192,13 @@ _HERE = contextlib.nullcontext()
 
 
 def _on(stream, device):
-    """The tensors' device as the current one for a call's launches."""
-    if stream is not None and stream.device != device:
-        raise ValueError(f"stream is on {stream.device}, the call's tensors on {device}")
+    """The tensors' device as the current one for a call's launches, and
+    `stream` as the current one for its allocations: memory freed on another
+    stream, whose kernels may still use it, is not handed out to this call."""
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"stream is on {stream.device}, the call's tensors on {device}")
+        return torch.cuda.stream(stream)
     return _HERE if torch._C._cuda_getDevice() == device.index else torch.cuda.device(device)
 
 
@@ -257,7 +264,7 @@ def act8_store(x, *, stream=None) -> Act8:
         rc = lib.qat_act8_store(_ptr(m), DTYPES[m.dtype], m.shape[0], m.shape[1], ld, _ptr(a.codes),
                                 _ptr(a.scales), _stream(stream, dev))
         _raise("qat_act8_store", rc)
-        _keep_alive(stream, a.codes, a.scales)
+    _keep_alive(stream, a.codes, a.scales)
     return a
 
 
@@ -281,7 +288,7 @@ def act8_load(a: Act8, dtype=None, *, out=None, stream=None):
         rc = lib.qat_act8_load(_ptr(a.codes), _ptr(a.scales), a.rows, a.cols, _ptr(out), DTYPES[dtype],
                                a.cols, _stream(stream, dev))
         _raise("qat_act8_load", rc)
-        _keep_alive(stream, out)
+    _keep_alive(stream, out)
     return out
 
 
@@ -310,7 +317,7 @@ def linear_act(x, W, bias=None, residual=None, activation="none", *, out=None, s
                                 N, K, _ptr(y), N, _ptr(z8.codes) if save else None,
                                 _ptr(z8.scales) if save else None, _ptr(ws), _size(ws), _stream(stream, dev))
         _raise("qat_linear_act", rc)
-        _keep_alive(stream, y, ws, *((z8.codes, z8.scales) if save else ()))
+    _keep_alive(stream, y, ws, *((z8.codes, z8.scales) if save else ()))
     return (y, z8) if save else y
 
 
@@ -351,7 +358,7 @@ def linear_act_vjp(dy, x8, W, z8=None, activation="none", *, want_dx=True, want_
                                     DTYPES[t], act, M, N, K, _ptr(dx), _ptr(dW), _ptr(db), _ptr(ws),
                                     _size(ws), _stream(stream, dev))
         _raise("qat_linear_act_vjp", rc)
-        _keep_alive(stream, dx, dW, db, ws)
+    _keep_alive(stream, dx, dW, db, ws)
     return dx, dW, db
 
 
@@ -389,12 +396,12 @@ def trellis_pack(states, state_bits: int, k: int, *, check=True, stream=None):
         rc = lib.trellis_pack(_ptr(states), B, steps, int(state_bits), int(k), _ptr(packed), _ptr(bad),
                               _stream(stream, dev))
         _raise("trellis_pack", rc)
-        _keep_alive(stream, packed, bad)
         if check:
             (torch.cuda.current_stream() if stream is None else stream).synchronize()
             n = int(bad.item())
             if n:
                 raise ValueError(f"{n} states are not those of a path with state_bits = {state_bits}, k = {k}")
+    _keep_alive(stream, packed)
     return packed
 
 
@@ -411,7 +418,7 @@ def trellis_unpack(packed, state_bits: int, k: int, steps: int, *, stream=None):
         rc = lib.trellis_unpack(_ptr(packed), math.prod(packed.shape[:-1]), steps, int(state_bits), int(k),
                                 _ptr(states), _stream(stream, dev))
         _raise("trellis_unpack", rc)
-        _keep_alive(stream, states)
+    _keep_alive(stream, states)
     return states
 
 
@@ -449,7 +456,7 @@ def trellis_dense(packed, codebook, state_bits: int, k: int, V: int = 1, block: 
         rc = lib.trellis_dense(_ptr(packed), B, _ptr(codebook), int(state_bits), int(k), int(V), int(block),
                                _ptr(scales), _ptr(W), DTYPES[dtype], _stream(stream, dev))
         _raise("trellis_dense", rc)
-        _keep_alive(stream, W)
+    _keep_alive(stream, W)
     return W
 
 
@@ -479,5 +486,5 @@ def trellis_linear(x, packed, codebook, state_bits: int, k: int, V: int = 1, blo
                                 int(block), _ptr(scales), _ptr(bias), _ptr(res), ldr, DTYPES[t], act, M, N, K,
                                 _ptr(y), N, _ptr(ws), _size(ws), _stream(stream, dev))
         _raise("trellis_linear", rc)
-        _keep_alive(stream, y, ws)
+    _keep_alive(stream, y, ws)
     return y

@@ -600,6 +600,79 @@ def test_other_streams():
         assert all(torch.equal(a, b) for a, b in zip(g, grads)) and torch.equal(v, Q.act8_load(want[1]))
 
 
+def _entry_points():
+    """Every entry point of the layer as a call of `stream`, at sizes whose
+    products are split and whose odd operands are padded, so that they take
+    workspaces."""
+    _, (x, W, b, r) = _layer(4, 300, 264, 4100, torch.bfloat16)
+    _, (xl, Wl, bl, rl) = _layer(5, 1500, 1501, 1003, torch.bfloat16)
+    x8, xl8 = Q.act8_store(x), Q.act8_store(xl)
+    z8, zl8 = (Q.linear_act(*a, None, "silu", save=True)[1] for a in ((x, W, b), (xl, Wl, bl)))
+    _, s, packed, cd, sd = _coded(3, 264, 4096, 10, 2, 1, 256)
+    states = Q.trellis_unpack(packed, 10, 2, 256)
+    xc = x[:, :4096].contiguous()
+    return {
+        "act8_store": lambda s: Q.act8_store(x, stream=s),
+        "act8_load": lambda s: Q.act8_load(x8, stream=s),
+        "linear_act": lambda s: Q.linear_act(x, W, b, r, "silu", stream=s),
+        "linear_act with a checkpoint": lambda s: Q.linear_act(x, W, b, r, "silu", save=True, stream=s),
+        "linear_act, padded": lambda s: Q.linear_act(xl, Wl, bl, rl, "silu", stream=s),
+        "linear_act_vjp": lambda s: Q.linear_act_vjp(r, x8, W, z8, "silu", stream=s),
+        "linear_act_vjp, padded": lambda s: Q.linear_act_vjp(rl, xl8, Wl, zl8, "silu", stream=s),
+        "trellis_pack": lambda s: Q.trellis_pack(states, 10, 2, check=False, stream=s),
+        "trellis_unpack": lambda s: Q.trellis_unpack(packed, 10, 2, 256, stream=s),
+        "trellis_dense": lambda s: Q.trellis_dense(packed, cd, 10, 2, scales=sd, stream=s),
+        "trellis_linear": lambda s: Q.trellis_linear(xc, packed, cd, 10, 2, scales=sd, bias=b, stream=s),
+    }
+
+
+def _tensors(out):
+    parts = out if isinstance(out, tuple) else (out,)
+    return [t for p in parts for t in ((p.codes, p.scales) if isinstance(p, Q.Act8) else (p,))]
+
+
+def test_calls_on_a_stream_allocate_from_its_pool(monkeypatch):
+    """What the current stream has freed, and may still be writing, is not what
+    a call on another stream gets for its outputs and its workspace."""
+    calls = _entry_points()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    asked, real = [], Q._space
+    monkeypatch.setattr(Q, "_space", lambda *a: asked.append(torch.cuda.current_stream()) or real(*a))
+    for name, call in calls.items():
+        _say(f"[pool] {name}")
+        first = _tensors(call(None))
+        want, freed = [t.clone() for t in first], {t.data_ptr() for t in first}
+        del first
+        torch.cuda.synchronize()
+        asked.clear()
+        got = _tensors(call(s))
+        s.synchronize()
+        assert not freed & {t.data_ptr() for t in got}, name
+        assert all(a == s for a in asked), name
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), name
+        assert torch.cuda.current_stream() != s
+
+
+def test_the_current_and_another_stream_at_once():
+    """Calls queued on the current stream behind long work, and the same on
+    another stream at once: neither touches the other's workspace."""
+    calls = _entry_points()
+    want = {name: [t.clone() for t in _tensors(call(None))] for name, call in calls.items()}
+    a = torch.randn(6144, 6144, device="cuda")
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for name, call in calls.items():
+        _say(f"[at once] {name}")
+        got = []
+        for _ in range(3):
+            torch.mm(a, a)
+            got += [_tensors(call(None)), _tensors(call(s))]
+        torch.cuda.synchronize()
+        for g in got:
+            assert all(torch.equal(p, q) for p, q in zip(g, want[name])), name
+
+
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_captured_calls_replay(M):
     """A layer's calls captured into a graph: several replays with new inputs
