@@ -33,6 +33,7 @@ The linear layer that trains and answers with the codewords is in
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 __all__ = [
@@ -173,6 +174,26 @@ def _keep_alive(stream, *tensors):
             t.record_stream(here)
 
 
+def _on_stream(call):
+    """An entry point that launches on `stream` also allocates there: with
+    `stream` as the current one its outputs and workspace come from that
+    stream's pool, so that memory freed on another stream, whose kernels may
+    still use it, is not handed out to this call.  Inputs have to be ready on
+    `stream` and live until it is done; the outputs may be used on the current
+    stream once that has waited for `stream`."""
+    @functools.wraps(call)
+    def entry(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        torch = _torch()
+        with torch.cuda.stream(stream):
+            out = call(*args, stream=stream, **kw)
+        parts = out if isinstance(out, tuple) else (out,)
+        _keep_alive(stream, *parts, kw.get("workspace"))
+        return out
+    return entry
+
+
 def _ws_bytes(ws):
     return ws.numel() * ws.element_size()
 
@@ -208,6 +229,7 @@ def _raise(fn, rc):
 
 
 # ---------------------------------------------------------------- API
+@_on_stream
 def bcjr_soft_codeword(w, codebook, state_bits, k, T, *, w_soft=None, logZ=None, want_logZ=True,
                        workspace=None, stream=None):
     """Soft codeword w_soft[B, L] and natural-log partition function logZ[B]."""
@@ -227,10 +249,10 @@ def bcjr_soft_codeword(w, codebook, state_bits, k, T, *, w_soft=None, logZ=None,
     rc = lib.bcjr_soft_codeword(_ptr(w), B, L, _ptr(codebook), state_bits, k, float(T),
                                 _ptr(w_soft), _ptr(logZ), _ptr(ws), _ws_bytes(ws), _stream(stream))
     _raise("bcjr_soft_codeword", rc)
-    _keep_alive(stream, w_soft, logZ, ws)
     return w_soft, logZ
 
 
+@_on_stream
 def bcjr_soft_codeword_vjp(w, codebook, state_bits, k, T, grad_w_soft, *, want_dW=True,
                            want_dCodebook=True, dW=None, dCodebook=None, workspace=None,
                            stream=None):
@@ -253,10 +275,10 @@ def bcjr_soft_codeword_vjp(w, codebook, state_bits, k, T, grad_w_soft, *, want_d
                                     _ptr(grad_w_soft), _ptr(dW), _ptr(dCodebook), _ptr(ws),
                                     _ws_bytes(ws), _stream(stream))
     _raise("bcjr_soft_codeword_vjp", rc)
-    _keep_alive(stream, dW, dCodebook, ws)
     return dW, dCodebook
 
 
+@_on_stream
 def bcjr_soft_codeword_fwd_vjp(w, codebook, state_bits, k, T, grad_w_soft, *, want_w_soft=True,
                                want_logZ=True, want_dW=True, want_dCodebook=True, w_soft=None,
                                logZ=None, dW=None, dCodebook=None, workspace=None, stream=None):
@@ -284,7 +306,6 @@ def bcjr_soft_codeword_fwd_vjp(w, codebook, state_bits, k, T, grad_w_soft, *, wa
                                         _ptr(grad_w_soft), _ptr(w_soft), _ptr(logZ), _ptr(dW),
                                         _ptr(dCodebook), _ptr(ws), _ws_bytes(ws), _stream(stream))
     _raise("bcjr_soft_codeword_fwd_vjp", rc)
-    _keep_alive(stream, w_soft, logZ, dW, dCodebook, ws)
     return w_soft, logZ, dW, dCodebook
 
 
@@ -310,6 +331,7 @@ def bcjr_soft_codeword_fwd_vjp_noalloc(w, codebook, state_bits, k, T, grad_w_sof
     return w_soft, logZ, dW, dCodebook
 
 
+@_on_stream
 def bcjr_ste_vjp(w, codebook, state_bits, k, T, w_hard, grad_w_soft, *, want_dW=True,
                  want_dCodebook=True, dW=None, dCodebook=None, workspace=None, stream=None):
     """Backward pass of BCJR-STE: the VJP of <grad_w_soft, w_soft> at temperature T,
@@ -334,10 +356,10 @@ def bcjr_ste_vjp(w, codebook, state_bits, k, T, w_hard, grad_w_soft, *, want_dW=
                           _ptr(grad_w_soft), _ptr(dW), _ptr(dCodebook), _ptr(ws), _ws_bytes(ws),
                           _stream(stream))
     _raise("bcjr_ste_vjp", rc)
-    _keep_alive(stream, dW, dCodebook, ws)
     return dW, dCodebook
 
 
+@_on_stream
 def viterbi_decode(w, codebook, state_bits, k, *, want_w_hard=True, states=None, w_hard=None,
                    workspace=None, stream=None):
     """Minimum-distortion path: (states[B, L] int32, w_hard[B, L] or None)."""
@@ -357,7 +379,6 @@ def viterbi_decode(w, codebook, state_bits, k, *, want_w_hard=True, states=None,
     rc = lib.viterbi_decode(_ptr(w), B, L, _ptr(codebook), state_bits, k, _ptr(states),
                             _ptr(w_hard), _ptr(ws), _ws_bytes(ws), _stream(stream))
     _raise("viterbi_decode", rc)
-    _keep_alive(stream, states, w_hard, ws)
     return states, w_hard
 
 
@@ -382,6 +403,7 @@ def _vec_workspace(workspace, B, L, state_bits, k, V, op, device):
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
+@_on_stream
 def bcjr_vec_soft_codeword(w, codebook, state_bits, k, V, T, *, w_soft=None, logZ=None,
                            want_logZ=True, workspace=None, stream=None):
     """Soft codeword w_soft[B, L] and logZ[B] with V weights per step."""
@@ -401,10 +423,10 @@ def bcjr_vec_soft_codeword(w, codebook, state_bits, k, V, T, *, w_soft=None, log
     rc = lib.bcjr_vec_soft_codeword(_ptr(w), B, L, _ptr(codebook), state_bits, k, V, float(T),
                                     _ptr(w_soft), _ptr(logZ), _ptr(ws), _ws_bytes(ws), _stream(stream))
     _raise("bcjr_vec_soft_codeword", rc)
-    _keep_alive(stream, w_soft, logZ, ws)
     return w_soft, logZ
 
 
+@_on_stream
 def bcjr_vec_soft_codeword_fwd_vjp(w, codebook, state_bits, k, V, T, grad_w_soft, *,
                                    want_w_soft=True, want_logZ=True, want_dW=True,
                                    want_dCodebook=True, w_soft=None, logZ=None, dW=None,
@@ -436,7 +458,6 @@ def bcjr_vec_soft_codeword_fwd_vjp(w, codebook, state_bits, k, V, T, grad_w_soft
                                             _ptr(dW), _ptr(dCodebook), _ptr(ws), _ws_bytes(ws),
                                             _stream(stream))
     _raise("bcjr_vec_soft_codeword_fwd_vjp", rc)
-    _keep_alive(stream, w_soft, logZ, dW, dCodebook, ws)
     return w_soft, logZ, dW, dCodebook
 
 
@@ -451,6 +472,7 @@ def bcjr_vec_soft_codeword_vjp(w, codebook, state_bits, k, V, T, grad_w_soft, *,
     return out[2], out[3]
 
 
+@_on_stream
 def bcjr_vec_viterbi_decode(w, codebook, state_bits, k, V, *, want_w_hard=True, states=None,
                             w_hard=None, workspace=None, stream=None):
     """(states[B, L // V] int32, w_hard[B, L] or None) with V weights per step."""
@@ -472,11 +494,11 @@ def bcjr_vec_viterbi_decode(w, codebook, state_bits, k, V, *, want_w_hard=True, 
     rc = lib.bcjr_vec_viterbi_decode(_ptr(w), B, L, _ptr(codebook), state_bits, k, V, _ptr(states),
                                      _ptr(w_hard), _ptr(ws), _ws_bytes(ws), _stream(stream))
     _raise("bcjr_vec_viterbi_decode", rc)
-    _keep_alive(stream, states, w_hard, ws)
     return states, w_hard
 
 
 # ---------------------------------------------------------------- training helpers
+@_on_stream
 def bcjr_gaussian_codebook(state_bits, V=1, seed=0, *, out=None, device="cuda", stream=None):
     """Computed Gaussian codebook: [S] (V = 1) or [S, V] float32 on the device."""
     torch = _torch()
@@ -490,7 +512,6 @@ def bcjr_gaussian_codebook(state_bits, V=1, seed=0, *, out=None, device="cuda", 
     rc = lib.bcjr_gaussian_codebook(_ptr(out), state_bits, V, int(seed) & ((1 << 64) - 1),
                                     _stream(stream))
     _raise("bcjr_gaussian_codebook", rc)
-    _keep_alive(stream, out)
     return out
 
 

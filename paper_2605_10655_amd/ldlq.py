@@ -24,7 +24,7 @@ import ctypes
 
 import torch
 
-from . import _check_in, _ptr, _raise, _stream, load_library
+from . import _check_in, _keep_alive, _ptr, _raise, _stream, load_library
 
 __all__ = ["block_ldl", "ldlq_viterbi", "hw_loss"]
 
@@ -54,13 +54,15 @@ def block_ldl(H: torch.Tensor, block: int, damp: float = 0.0, want_D: bool = Tru
     if H.dim() != 2 or H.shape != (d, d) or d % block:
         raise ValueError("H must be square with a size that is a multiple of block")
     _check_in("H", H)
-    M = torch.empty((d, d), dtype=torch.float64, device=H.device)
-    D = torch.empty((d, d), dtype=torch.float64, device=H.device) if want_D else None
     nbytes = lib.bcjr_block_ldl_workspace_bytes(d, block)
-    ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=H.device)
-    rc = lib.bcjr_block_ldl(_ptr(H), d, block, float(damp), _ptr(M), _ptr(D), _ptr(ws), ws.numel(),
-                            _stream(stream))
+    with torch.cuda.stream(stream):   # allocations from the pool of the launches' stream
+        M = torch.empty((d, d), dtype=torch.float64, device=H.device)
+        D = torch.empty((d, d), dtype=torch.float64, device=H.device) if want_D else None
+        ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=H.device)
+        rc = lib.bcjr_block_ldl(_ptr(H), d, block, float(damp), _ptr(M), _ptr(D), _ptr(ws), ws.numel(),
+                                _stream(stream))
     _raise("bcjr_block_ldl", rc)
+    _keep_alive(stream, M, D, ws)
     return M, D
 
 
@@ -88,15 +90,17 @@ def ldlq_viterbi(W, codebook, state_bits: int, k: int, H, block: int = 256, V: i
     if codebook.numel() != (1 << state_bits) * V:
         raise ValueError("codebook must hold 2^state_bits x V values")
     nb = cols // block
-    W_hat = torch.empty_like(W)
-    states = torch.empty((nb, rows, block // V), dtype=torch.int32, device=dev)
-    targets = torch.empty((nb, rows, block), dtype=W.dtype, device=dev) if return_targets else None
     nbytes = lib.bcjr_ldlq_workspace_bytes(rows, cols, block, state_bits, k, V)
     if nbytes == 0:
         raise ValueError("unsupported shape for the BlockLDLQ decode")
-    ws = torch.empty(int(nbytes), dtype=torch.uint8, device=dev)
-    rc = lib.bcjr_ldlq_viterbi(_ptr(W), rows, cols, _ptr(codebook), state_bits, k, V, _ptr(H), block,
-                               float(damp), _ptr(W_hat), _ptr(states), _ptr(targets), _ptr(ws),
-                               ws.numel(), _stream(stream))
+    with torch.cuda.stream(stream):   # allocations from the pool of the launches' stream
+        W_hat = torch.empty_like(W)
+        states = torch.empty((nb, rows, block // V), dtype=torch.int32, device=dev)
+        targets = torch.empty((nb, rows, block), dtype=W.dtype, device=dev) if return_targets else None
+        ws = torch.empty(int(nbytes), dtype=torch.uint8, device=dev)
+        rc = lib.bcjr_ldlq_viterbi(_ptr(W), rows, cols, _ptr(codebook), state_bits, k, V, _ptr(H), block,
+                                   float(damp), _ptr(W_hat), _ptr(states), _ptr(targets), _ptr(ws),
+                                   ws.numel(), _stream(stream))
     _raise("bcjr_ldlq_viterbi", rc)
+    _keep_alive(stream, W_hat, states, targets, ws)
     return (W_hat, states, targets) if return_targets else (W_hat, states)
