@@ -151,9 +151,11 @@ def anneal_qat(W_init, codebook, cfg: QATConfig, target=None, H=None, stream=Non
         # one asked for, and order it with the caller's on both sides
         here = torch.cuda.current_stream(stream.device)
         stream.wait_stream(here)
-        with torch.cuda.stream(stream):
-            res = anneal_qat(W_init, codebook, cfg, target, H, None, X, bias, activation)
-        here.wait_stream(stream)
+        try:
+            with torch.cuda.stream(stream):
+                res = anneal_qat(W_init, codebook, cfg, target, H, None, X, bias, activation)
+        finally:   # a run that ends early too: the caller may then free the inputs
+            here.wait_stream(stream)
         for t in (res.W, res.codebook, res.W_hard, res.packed):
             if t is not None:
                 t.record_stream(here)

@@ -90,3 +90,24 @@ def test_given_outputs_and_workspace_are_used():
     got, logZ = P.bcjr_soft_codeword(w, c, n, k, T, w_soft=out, workspace=ws, stream=s)
     s.synchronize()
     assert got is out and torch.equal(out, want[0]) and torch.equal(logZ, want[1])
+
+
+def test_a_run_that_ends_early_is_waited_for(monkeypatch):
+    """anneal_qat on another stream, ended by an error: the caller's stream is
+    ordered behind what was queued, as the inputs may be freed next."""
+    from paper_2605_10655_amd import qat
+    s, here = torch.cuda.Stream(), torch.cuda.current_stream()
+    waits, real = [], torch.cuda.Stream.wait_stream
+    monkeypatch.setattr(torch.cuda.Stream, "wait_stream", lambda a, b: waits.append((a, b)) or real(a, b))
+
+    def ends(*a, **kw):
+        raise RuntimeError("ended")
+
+    monkeypatch.setattr(qat, "qat_adam_step", ends)
+    g = torch.Generator().manual_seed(1)
+    W, c = torch.randn(4, 32, generator=g).cuda(), torch.randn(16, generator=g).cuda()
+    cfg = qat.QATConfig(state_bits=4, k=2, block=16, steps=2, T0=0.2, T_end=0.1)
+    with pytest.raises(RuntimeError, match="ended"):
+        qat.anneal_qat(W, c, cfg, stream=s)
+    assert waits == [(s, here), (here, s)]
+    torch.cuda.synchronize()
