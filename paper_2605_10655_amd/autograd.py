@@ -117,7 +117,8 @@ class LinearAct8(torch.autograd.Function):
         y, z8 = out if need_z else (out, None)
         if need_W and x8 is None:
             x8 = act8_store(x)
-        ctx.activation, ctx.x_shape = activation, x.shape
+        ctx.activation = activation
+        ctx.residual_shape = residual.shape if need_r else None
         ctx.rows, ctx.cols, ctx.dtype = x.numel() // max(x.shape[-1], 1), x.shape[-1], x.dtype
         ctx.save_for_backward(W if need_x else None, *((x8.codes, x8.scales) if need_W else (None, None)),
                               *((z8.codes, z8.scales) if need_z else (None, None)))
@@ -133,7 +134,8 @@ class LinearAct8(torch.autograd.Function):
         z8 = Act8(zc, zs, ctx.rows, torch.float32) if zc is not None else None
         dx, dW, db = linear_act_vjp(g, x8, W, z8, ctx.activation if z8 is not None else "none",
                                     want_dx=need_x, want_dW=need_W, want_dbias=need_b)
-        return dx, dW, db, dy if need_r else None, None, None
+        # (a residual [M, N] beside an x of more dimensions, or the reverse)
+        return dx, dW, db, dy.reshape(ctx.residual_shape) if need_r else None, None, None
 
 
 def linear_act8(x, W, bias=None, residual=None, activation="none", x8=None):

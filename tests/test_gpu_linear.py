@@ -737,6 +737,19 @@ def test_autograd_gives_the_calls_gradients():
         linear_act8(devi[0][:3], devi[1], x8=x8)
 
 
+def test_gradients_of_a_residual_of_another_shape():
+    _, (x, W, b, r) = _layer(3, 70, 40, 96, torch.bfloat16)
+    dy = torch.randn(70, 40, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    leaves = [t.clone().requires_grad_() for t in (x, W, b, r)]
+    linear_act8(*leaves, "gelu").backward(dy)
+    for xs, rs in (((7, 10, 96), (70, 40)), ((70, 96), (2, 35, 40)), ((5, 14, 96), (10, 7, 40))):
+        parts = [t.clone().requires_grad_() for t in (x.view(xs), W, b, r.view(rs))]
+        y = linear_act8(*parts, "gelu")
+        y.backward(dy.view(y.shape))
+        for p, q in zip(parts, leaves):
+            assert torch.equal(p.grad, q.grad.view(p.shape))
+
+
 def _padded_layer():
     _, (x, W, b, r) = _layer(5, 96, 40, 64, torch.bfloat16)
     return x, W, b, r

@@ -162,6 +162,25 @@ def test_host_tensors_are_refused(lib):
         linear_act8(x.requires_grad_(), W)
 
 
+@pytest.mark.parametrize("xs,rs", [((2, 3, 4), (6, 5)), ((6, 4), (2, 3, 5)), ((2, 3, 4), (2, 3, 5)), ((1, 4), (1, 1, 5))])
+def test_residual_of_another_shape_gets_its_gradient(xs, rs, monkeypatch):
+    """linear_act takes any shapes of as many rows; the residual's gradient has
+    the residual's.  (On the host: the product itself is plain here.)"""
+    from paper_2605_10655_amd import autograd as A
+
+    def product(x, W, bias, residual, activation, save=False):
+        return (x.flatten(0, -2) @ W.t() + residual.flatten(0, -2)).view(*x.shape[:-1], W.shape[0])
+
+    monkeypatch.setattr(A, "linear_act", product)
+    monkeypatch.setattr(A, "linear_act_vjp", lambda *a, **kw: (None, None, None))
+    x, W = torch.randn(xs), torch.randn(5, 4)
+    r = torch.randn(rs, requires_grad=True)
+    y = A.linear_act8(x, W, None, r)
+    dy = torch.randn(y.shape)
+    y.backward(dy)
+    assert r.grad.shape == r.shape and torch.equal(r.grad.flatten(), dy.flatten())
+
+
 def test_anneal_refuses_what_a_layer_loss_cannot_take():
     from paper_2605_10655_amd.qat import QATConfig, anneal_qat
     cfg = QATConfig(state_bits=4, k=2, block=16)
