@@ -311,7 +311,9 @@ int qat_act8_load(const int8_t *codes, const uint16_t *scales, int64_t rows, int
  * bias [N] or NULL, residual [M, N] or NULL, y [M, N].  z_codes and z_scales
  * (both or neither) receive the 8-bit checkpoint of z, taken from the fp32
  * sums (as for dtype QAT_F32).  M == 0 is a no-op.  Workspace:
- * qat_linear_act_workspace_bytes() bytes, 16-byte aligned (NULL where 0). */
+ * qat_linear_act_workspace_bytes() bytes, 16-byte aligned (NULL where 0, and
+ * for up to QAT_FEW_TOKENS tokens without a checkpoint). */
+#define QAT_FEW_TOKENS 16
 size_t qat_linear_act_workspace_bytes(int dtype, int64_t M, int64_t N, int64_t K);
 int qat_linear_act(const void *x, int64_t ldx, const void *W, int64_t ldw, const void *bias,
                    const void *residual, int64_t ldr, int dtype, int activation, int64_t M, int64_t N,

@@ -307,10 +307,10 @@ int qat_linear_act(const void* x, int64_t ldx, const void* W, int64_t ldw, const
   if (!x || !W || !y || misaligned(x, es) || misaligned(W, es) || misaligned(y, es) || misaligned(bias, es) ||
       misaligned(residual, es) || misaligned(z_codes, 16) || misaligned(z_scales, 2))
     return BCJR_ERR_INVALID_ARG;
+  if (M <= QAT_FEW_TOKENS && !z_codes)   // (before the plan of a product that is not launched)
+    return run_few(few_args(x, ldx, bias, residual, ldr, y, ldy, activation, M, N, K), W, ldw, dtype, stream);
   const size_t need = qat_linear_act_workspace_bytes(dtype, M, N, K);
   if (need && (!workspace || misaligned(workspace, 16) || ws_bytes < need)) return BCJR_ERR_WORKSPACE;
-  if (M <= 16 && !z_codes)
-    return run_few(few_args(x, ldx, bias, residual, ldr, y, ldy, activation, M, N, K), W, ldw, dtype, stream);
   const GemmArgs g = {x, W, ldx, ldw, nullptr, M, N, K, bias, residual, ldr, y, ldy, z_codes, z_scales, activation};
   return run_linear(g, dtype, static_cast<char*>(workspace), stream);
 }

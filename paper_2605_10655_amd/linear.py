@@ -46,6 +46,7 @@ __all__ = ["ACTIVATIONS", "Act8", "act8_store", "act8_load", "linear_act", "line
 ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "gelu_tanh": 3}
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 GROUP = 32   # rows (tokens) of an 8-bit group
+FEW = 16     # tokens whose product needs no workspace unless it keeps a checkpoint
 
 
 def _lib():
@@ -312,7 +313,7 @@ def linear_act(x, W, bias=None, residual=None, activation="none", *, out=None, s
     with _on(stream, dev):
         y = _output("out", out, (*x.shape[:-1], N), m, w, bias, res)
         z8 = _new_act8(M, N, torch.float32, dev) if save else None
-        ws = _space(workspace, _linear_bytes(DTYPES[t], M, N, K), dev)
+        ws = _space(workspace, 0 if M <= FEW and not save else _linear_bytes(DTYPES[t], M, N, K), dev)
         rc = lib.qat_linear_act(_ptr(m), ldx, _ptr(w), ldw, _ptr(bias), _ptr(res), ldr, DTYPES[t], act, M,
                                 N, K, _ptr(y), N, _ptr(z8.codes) if save else None,
                                 _ptr(z8.scales) if save else None, _ptr(ws), _size(ws), _stream(stream, dev))

@@ -176,6 +176,28 @@ def test_linear_of_no_tokens_and_of_three_dimensions():
 
 
 @pytest.mark.parametrize("t", R.TYPES)
+@pytest.mark.parametrize("M", [1, 16])
+def test_a_few_tokens_need_no_workspace(t, M, monkeypatch):
+    """Neither from Python, which does not ask for its size, nor from C, where
+    a product of so long a sum would have one; with a checkpoint it still does."""
+    dt = R.TYPES[t]
+    host, (x, W, b, r) = _layer(M, M, 72, 20000, dt)
+    y, yb, _, _ = R.linear64(*host, "silu", dt)
+    lib, s = Q._lib(), torch.cuda.current_stream().cuda_stream
+    assert lib.qat_linear_act_workspace_bytes(Q.DTYPES[dt], M, 72, 20000) > 0
+    out, z8 = torch.empty_like(r), Q._new_act8(M, 72, torch.float32, x.device)
+    args = [x.data_ptr(), 20000, W.data_ptr(), 20000, b.data_ptr(), r.data_ptr(), 72, Q.DTYPES[dt], 1, M, 72, 20000,
+            out.data_ptr(), 72]
+    assert lib.qat_linear_act(*args, None, None, None, 0, s) == 0
+    within(out, y, yb, f"{t} M={M}")
+    assert lib.qat_linear_act(*args, z8.codes.data_ptr(), z8.scales.data_ptr(), None, 0, s) == -3
+    monkeypatch.setattr(Q, "_linear_bytes", None)
+    assert torch.equal(Q.linear_act(x, W, b, r, "silu"), out)
+    with pytest.raises(TypeError):
+        Q.linear_act(x, W, b, r, "silu", save=True)
+
+
+@pytest.mark.parametrize("t", R.TYPES)
 def test_non_finite_values_stay_in_their_rows(t):
     """A padded row's infinities and NaN reach that row's outputs alone, and
     in the checkpoint that row's codes alone."""
