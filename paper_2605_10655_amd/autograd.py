@@ -22,8 +22,6 @@ the checkpoint's z; everything else is exact up to rounding.
 """
 from __future__ import annotations
 
-import weakref
-
 import torch
 
 from . import bcjr_soft_codeword, bcjr_soft_codeword_vjp, bcjr_ste_vjp, viterbi_decode
@@ -84,25 +82,25 @@ def bcjr_quant(W, codebook, state_bits: int, k: int, T, block: int = 256, hard: 
     return out.reshape(W.shape)
 
 
-# LinearAct8's nodes of graphs recorded eagerly on a device's default stream.
-_EAGER = weakref.WeakSet()
-
-
-def _note_leaves(ctx, tensors):
+def _note_leaves(ctx, x):
     """Refuses to capture a layer while an eager graph over the same leaves
-    lives.  The leaf's gradient is accumulated on the stream that the older
-    graph was recorded on; where that is the default stream, a captured
-    backward pass would order it behind the capture, which ends the process."""
-    ids = frozenset(id(t) for t, need in zip(tensors, ctx.needs_input_grad) if need and t.is_leaf)
-    if not ids or not tensors[0].is_cuda:   # (linear_act refuses the latter)
+    lives.  A leaf's gradient is accumulated on the stream that its
+    accumulation node was made on; where that is the default stream, a captured
+    backward pass would order it behind the capture, which ends the process.
+    The node lives as long as any graph over the leaf does, so it carries the
+    mark itself."""
+    if not x.is_cuda:   # (linear_act refuses it)
+        return
+    leaves = [n for n, _ in ctx.next_functions if n is not None and hasattr(n, "variable")]
+    if not leaves:
         return
     if torch.cuda.is_current_stream_capturing():
-        if any(not ids.isdisjoint(node.leaves) for node in list(_EAGER)):
+        if any("linear_act8 on the default stream" in n.metadata for n in leaves):
             raise RuntimeError("linear_act8 is being captured while the result of an eager call on the same "
                                "leaves lives: drop that result first, or run it on a stream of its own")
-    elif torch.cuda.current_stream(tensors[0].device).cuda_stream == 0:
-        ctx.leaves = ids
-        _EAGER.add(ctx)
+    elif torch.cuda.current_stream(x.device).cuda_stream == 0:
+        for n in leaves:
+            n.metadata["linear_act8 on the default stream"] = True
 
 
 class LinearAct8(torch.autograd.Function):
@@ -110,7 +108,7 @@ class LinearAct8(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, W, bias, residual, activation, x8):
-        _note_leaves(ctx, (x, W, bias, residual))
+        _note_leaves(ctx, x)
         need_x, need_W, need_b, need_r = ctx.needs_input_grad[:4]
         need_z = activation != "none" and (need_x or need_W or need_b)
         out = linear_act(x, W, bias, residual, activation, save=need_z)

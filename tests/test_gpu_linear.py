@@ -831,6 +831,31 @@ def test_capture_over_the_leaves_of_a_living_graph_is_refused(monkeypatch):
     assert linear_act8(x, W, b) is not None and kept is not None and z is not None
 
 
+def test_capture_is_refused_as_long_as_the_leafs_node_lives(monkeypatch):
+    """The node that accumulates a leaf's gradient outlives the result that it
+    was made for while another graph over the leaf lives, on whatever stream;
+    no other caller's leaves count.  (Without a capture.)"""
+    x, W, b, r = _padded_layer()
+    W = W.requires_grad_()
+    first = linear_act8(x, W, b, r, "gelu")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        second = linear_act8(x, W, b, r, "gelu")
+    torch.cuda.current_stream().wait_stream(side)
+    del first
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError):
+        linear_act8(x, W)
+    del second
+    assert linear_act8(x, W) is not None
+    monkeypatch.undo()
+    with torch.cuda.stream(side):
+        third = linear_act8(x, W, b, r, "gelu")
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    assert linear_act8(x, W) is not None and third is not None
+
+
 def test_no_gradient_keeps_no_checkpoint(monkeypatch):
     x, W, b, r = _padded_layer()
     W = W.requires_grad_()
