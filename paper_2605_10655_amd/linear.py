@@ -35,6 +35,7 @@ import ctypes
 import dataclasses
 import functools
 import math
+import operator
 
 import torch
 
@@ -364,9 +365,11 @@ def linear_act_vjp(dy, x8, W, z8=None, activation="none", *, want_dx=True, want_
 
 
 # ---------------------------------------------------------------- trellis codes
-@functools.lru_cache(maxsize=1024)
+@functools.lru_cache(maxsize=1024, typed=True)
 def _code(state_bits, k, V, block):
-    words = int(_lib().trellis_words(int(state_bits), int(k), int(V), int(block)))
+    state_bits, k, V, block = map(operator.index, (state_bits, k, V, block))   # whole numbers: nothing is cut off
+    few = max(state_bits, k, V, block) < 1 << 31   # (C's ints would wrap)
+    words = int(_lib().trellis_words(state_bits, k, V, block)) if few else 0
     if words == 0:
         raise ValueError(f"no trellis code for state_bits = {state_bits}, k = {k}, V = {V}, "
                          f"block = {block}: 1 <= k <= state_bits <= 16, 1 <= V <= 8, V divides block")

@@ -145,6 +145,16 @@ def test_small_layers_need_no_workspace(lib):
     assert need(1, 17, 4096, 4096, 12, 2, 1, 256) > 0 and need(1, 65, 256, 256, 12, 2, 1, 256) > 0
 
 
+def test_a_trellis_is_given_by_whole_numbers(lib):
+    assert Q.trellis_words(np.int64(16), 2, np.int32(1), 256) == 17
+    for args in ((16.5, 2), (16.0, 2), (16, 2.5), (16, 2, 1.5), (16, 2, 1, 256.5), ("16", 2)):
+        with pytest.raises(TypeError):
+            Q.trellis_words(*args)
+    for args in (((1 << 32) + 16, 2), (16, (1 << 32) + 2), (16, 2, (1 << 32) + 1), (16, 2, 1, (1 << 64) + 256), (16, -2)):
+        with pytest.raises(ValueError):
+            Q.trellis_words(*args)
+
+
 def test_host_tensors_are_refused(lib):
     x, W = torch.zeros(4, 8), torch.zeros(6, 8)
     for call in (lambda: Q.act8_store(x), lambda: Q.linear_act(x, W), lambda: Q.linear_act_vjp(x, None, W),
