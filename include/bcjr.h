@@ -277,13 +277,14 @@ int qat_sgd_step(float *param, const float *grad, int64_t count, float lr, float
  * Types and activations.  dtype is the type of x, W, bias, residual, y, their
  * gradients and of the matrix instructions' operands; every sum is held in
  * fp32.  Matrices are row-major with a leading dimension in elements (ldx >=
- * columns); pointers are aligned to their element, codes to 16 bytes.  Inputs
- * and outputs must not overlap, nor the workspaces of calls that may run at
- * the same time.  Rows up to 2^31 - 1, columns up to 2^22 - 1, leading
- * dimensions of x, W and dy below 32 MiB, and below 2^32 threads a launch (of
- * which one covers at least 32 values, in trellis_pack, _unpack and _dense one
- * state), else BCJR_ERR_UNSUPPORTED.  Every call gives the same bits each
- * time; how many tokens share a call may change an output's last bits. */
+ * columns); pointers are aligned to their element, codes and codebook to 16
+ * bytes.  Inputs and outputs must not overlap, nor the workspaces of calls
+ * that may run at the same time.  Rows up to 2^31 - 1, columns up to 2^22 - 1,
+ * leading dimensions of x, W and dy below 32 MiB, and below 2^32 threads a
+ * launch (of which one covers at least 32 values, in trellis_pack, _unpack and
+ * _dense one state), else BCJR_ERR_UNSUPPORTED.  Every call gives the same
+ * bits each time; how many tokens share a call may change an output's last
+ * bits. */
 #define QAT_F32 0
 #define QAT_BF16 1
 #define QAT_F16 2

@@ -18,15 +18,16 @@ their trellis paths (``trellis_pack``), for one token as for a prompt.
 This module checks arguments, allocates outputs and workspaces and passes
 device pointers to the library's C ABI; every step runs in its HIP kernels.
 Tensors are float32, bfloat16 or float16, the same for every operand of a
-call.  Matrices may have a row stride (columns contiguous, rows not
+call. Matrices may have a row stride (columns contiguous, rows not
 overlapping); x, residual and dy may have more than two dimensions if they are
-contiguous.  Calls run on the tensors' device, on its current stream or
-`stream`; outputs and workspaces come from PyTorch's allocator, from the pool
-of the stream that the call runs on, so that no two streams share a workspace
-and calls captured into a graph own theirs.  On `stream` the inputs have to be
-ready, and live until it is done; what comes back may be used on the current
-stream once that has waited for `stream`.  The autograd node is
-``autograd.linear_act8``.
+contiguous. A codebook (float32) and an Act8's codes are aligned to 16 bytes,
+everything else to its element. Calls run on the tensors' device, on its
+current stream or `stream`; outputs and workspaces come from PyTorch's
+allocator, from the pool of the stream that the call runs on, so that no two
+streams share a workspace and calls captured into a graph own theirs. On
+`stream` the inputs have to be ready, and live until it is done; what comes
+back may be used on the current stream once that has waited for `stream`. The
+autograd node is ``autograd.linear_act8``.
 """
 from __future__ import annotations
 
@@ -242,6 +243,8 @@ def _check_act8(name, a, rows=None, cols=None, dtype=None, device=None):
         raise ValueError(f"{name}.scales must be {tuple(a.codes.shape[:2])}, got {tuple(a.scales.shape)}")
     if not a.codes.is_contiguous() or not a.scales.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    if a.codes.data_ptr() % 16:
+        raise ValueError(f"{name}.codes must be aligned to 16 bytes")
     if (rows is not None and a.rows != rows) or (cols is not None and a.cols != cols):
         raise ValueError(f"{name} must hold [{rows}, {cols}], it holds [{a.rows}, {a.cols}]")
     if dtype is not None and a.dtype != dtype:
@@ -437,6 +440,8 @@ def _packed(packed, codebook, scales, state_bits, k, V, block, device=None):
     S = 1 << state_bits
     if tuple(codebook.shape) not in (((S,), (S, 1)) if V == 1 else ((S, V),)) or not codebook.is_contiguous():
         raise ValueError(f"codebook must be contiguous with {S} x {V} values, got {tuple(codebook.shape)}")
+    if codebook.data_ptr() % 16:
+        raise ValueError("codebook must be aligned to 16 bytes: this view of a larger tensor is not, copy it")
     B = math.prod(packed.shape[:-1])
     if scales is not None:
         _tensor("scales", scales, torch.float32, dev)

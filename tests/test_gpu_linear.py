@@ -605,6 +605,27 @@ def test_refusals():
         Q.trellis_linear(x, packed, cb, **ok, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
 
 
+def test_a_codebook_out_of_line_is_refused_by_name():
+    """A view that does not begin at 16 bytes; one that does is taken."""
+    _, s, packed, cd, sd = _coded(5, 12, 64, 8, 2, 1, 32)
+    x = torch.ones(3, 64, device="cuda")
+    want = Q.trellis_linear(x, packed, cd, 8, 2, 1, 32)
+    for off in (1, 2, 3, 4):
+        view = torch.zeros(264, device="cuda")[off:off + 256]
+        view.copy_(cd)
+        if off % 4:
+            for call in (lambda: Q.trellis_linear(x, packed, view, 8, 2, 1, 32),
+                         lambda: Q.trellis_dense(packed, view, 8, 2, 1, 32)):
+                with pytest.raises(ValueError, match="16 bytes"):
+                    call()
+        else:
+            assert torch.equal(Q.trellis_linear(x, packed, view, 8, 2, 1, 32), want)
+    a = Q.act8_store(x)
+    codes = torch.zeros(a.codes.numel() + 8, dtype=torch.int8, device="cuda")[8:].view(a.codes.shape)
+    with pytest.raises(ValueError, match="16 bytes"):
+        Q.act8_load(Q.Act8(codes, a.scales, a.rows, a.dtype))
+
+
 # ---------------------------------------------------------------- streams, graphs, autograd
 def test_other_streams():
     host, devi = _layer(9, 200, 300, 500, torch.bfloat16)
