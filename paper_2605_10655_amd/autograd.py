@@ -147,8 +147,8 @@ def linear_act8(x, W, bias=None, residual=None, activation="none", x8=None):
         if not isinstance(x8, Act8):
             raise TypeError("x8 must be an Act8")
         rows = x.numel() // max(x.shape[-1], 1)
-        if (x8.rows, x8.cols, x8.dtype) != (rows, x.shape[-1], x.dtype):
-            raise ValueError("x8 is not a checkpoint of x: its size or type differs")
+        if (x8.rows, x8.cols, x8.dtype, x8.codes.device) != (rows, x.shape[-1], x.dtype, x.device):
+            raise ValueError("x8 is not a checkpoint of x: its size, type or device differs")
     if not torch.is_grad_enabled():   # nothing to keep for a backward pass
         return linear_act(x, W, bias, residual, activation)
     return LinearAct8.apply(x, W, bias, residual, activation, x8)

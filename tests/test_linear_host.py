@@ -191,6 +191,15 @@ def test_residual_of_another_shape_gets_its_gradient(xs, rs, monkeypatch):
     assert r.grad.shape == r.shape and torch.equal(r.grad.flatten(), dy.flatten())
 
 
+def test_a_checkpoint_on_another_device_is_refused_before_the_backward_pass():
+    from paper_2605_10655_amd.autograd import linear_act8
+    x, W = torch.zeros(4, 8), torch.zeros(6, 8, requires_grad=True)
+    a = Q.Act8(torch.zeros(1, 8, 32, dtype=torch.int8, device="meta"), torch.zeros(1, 8, dtype=torch.bfloat16), 4,
+               torch.float32)
+    with pytest.raises(ValueError, match="device"):
+        linear_act8(x, W, x8=a)
+
+
 def test_anneal_refuses_what_a_layer_loss_cannot_take():
     from paper_2605_10655_amd.qat import QATConfig, anneal_qat
     cfg = QATConfig(state_bits=4, k=2, block=16)
