@@ -298,8 +298,8 @@ int qat_sgd_step(float *param, const float *grad, int64_t count, float lr, float
  * which amax <= 127 * 2^e (e >= -126, for fp16 e >= -24), value v is held as
  *     q = round-half-even(v / 2^e)
  * (|q| <= 63 at e = 122, for fp16 at e = 10, where 64 would overflow the
- * type) and read back as q * 2^e: at most half a step 2^e off, exact in the
- * type.  codes is [ceil(rows / 32), cols, 32] int8, the last group's missing
+ * type) and read back as q * 2^e: at most half a step 2^e off (a value whose
+ * code is cut at 63 less than a step), exact in the type.  codes is [ceil(rows / 32), cols, 32] int8, the last group's missing
  * rows 0; scales is [ceil(rows / 32), cols], the bf16 bits of 2^e.  A
  * non-finite value is held as -128, reads back as NaN, does not count towards
  * amax, and makes its group's scale negative. */

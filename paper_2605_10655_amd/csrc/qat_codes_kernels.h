@@ -49,7 +49,13 @@ constexpr size_t codes_table(int n) {
   return (((size_t)sizeof(T) * V) << (n < kTableBits<T, V> ? n : kTableBits<T, V>)) / 16 * 16 + 32;
 }
 
-// Part h of the codebook as T, four values at a time.
+// Part h of the codebook as T, four values at a time.  The weights are the
+// matrix instructions' operands, so they are rounded to T here, half a step
+// each (their scale is applied to the fp32 sums): unrounded ones would take twice
+// the table and so twice the passes over the bit strings.  An output's error
+// against 64 bits is that of torch's product with weights in T, or less: bf16,
+// one token 2048 -> 8192, 2.4e-3 of the outputs' norm (torch 3.2e-3; of an output
+// rounded once 1.7e-3), 16 tokens 2048 -> 2048 2.4e-3 (2.4e-3).
 template <class T, int V>
 __device__ __forceinline__ void fill_table(T* table, const float* codebook, int n, int h, int tid, int threads) {
   const int count = V << (n < kTableBits<T, V> ? n : kTableBits<T, V>);
@@ -74,7 +80,9 @@ __device__ __forceinline__ void fill_table(T* table, const float* codebook, int 
 
 // (One workgroup fills a CU's LDS: four waves a SIMD and their 128 registers,
 // which the compiler would otherwise not all use to keep loads under way: 16.2
-// us against 14.5 for the second of the two above.)
+// us against 14.5 for the second of the two above.  For 17 to 64 tokens that is
+// too few: of the forms with 1 to 4 bits a step the fp32 ones keep up to 21
+// registers in scratch, the 16-bit ones 2 and 16 at 3 and 4.)
 template <class T, int KB, int V, int MT, int Q>
 __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(4, 4))) void codes_kernel(
     CodesArgs a) {
@@ -195,7 +203,9 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
 }
 
 // W = scale * codebook[state] of many weights, the product in fp32, rounded to
-// T.  A thread takes eight weights (16 bytes of a 16-bit type) in each of eight
+// T once, as the next product's operand (the error of the whole is 2.1e-3 of the
+// outputs' norm in bf16, 2048 tokens 8192 -> 2048; torch's product of weights
+// in bf16 2.6e-3, of an output rounded once 1.7e-3).  A thread takes eight weights (16 bytes of a 16-bit type) in each of eight
 // rows of 8192, kept in registers while the fp32 codebook passes through LDS in
 // pieces of 128 KB; of each, states of the others read a zero.  (Read from L2
 // a weight costs 1.1 cycles a CU and requests 64 bytes for 4: 16.8 million

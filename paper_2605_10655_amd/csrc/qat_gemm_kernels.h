@@ -529,9 +529,10 @@ __device__ __forceinline__ void finish(const GemmArgs& g, int part, f32x16 (&acc
 // under way (codes always so, becoming T on the way).  No step has a branch:
 // what is left of k beyond whole steps goes first, and steps past the last
 // fetch that one again, into buffers that nothing reads any more.  Tiles of 64
-// are bound by the matrix instructions in fp32 (500 tokens, 1024 -> 2048: 25
-// us; eight waves in turns, as below, take as long) and by a step's latency in
-// 16 bits (fp16 through registers, 333 tokens, 777 -> 1000: 12 us).
+// leave the matrix instructions idle 0.4 of the time in fp32, while a SIMD's
+// one wave reads its operands (500 tokens, 1024 -> 2048: 22 us; eight waves in
+// turns, as below, take as long), and are bound by a step's latency in 16 bits
+// (fp16 through registers, 333 tokens, 777 -> 1000: 11 us).
 template <class T, int AM, int BM, int BT, bool COPY>
 __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
   constexpr int kThreads = 256, W = BT / 2, NT = W / 32;
@@ -649,7 +650,9 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
       if constexpr (!kCopyB) TB::put(rb[slot], lds + TA::kChunks, tid);
     };
     // Two steps' copies, and the codes loaded after them, may be under way when
-    // a step's copies have landed.
+    // a step's copies have landed.  (A run of codes is two loads, its codes and
+    // its scale, and counts as one here: with codes the wait is for more than the
+    // step needs, never for less.)
     constexpr int kD = (kCopyA ? TA::kPer : 0) + (kCopyB ? TB::kPer : 0);
     constexpr int kF = kCopyA && !kCopyB ? TB::kLoads : 0;
     // Step s from `now`; `last` (read by every wave in step s - 1) receives step
@@ -706,11 +709,13 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g, int ti, int tj) {
 // waves read a tile is a reading one of the second four's: by its end every
 // wave has seen its copies of that tile land.
 //
-// 8192 cubed: bf16 781 us (1.41 PFLOP/s; the library's product 784), dx 803, dW
-// 900; fp32 7.55 ms (146 TFLOP/s, the library 153), dx 7.65, dW 8.3.  Bound by
-// the matrix instructions at the clock that they leave.  4096 tokens, 2048 ->
-// 8192 with SiLU and a checkpoint take 146 us, 33 of them the two epilogues:
-// all workgroups write at once (100 MB) and none multiplies.
+// 8192 cubed on one card: bf16 769 us (1.43 PFLOP/s; the library's product 698,
+// on others 781 and 784, 791 and 870), dx 781, dW 775; fp32 7.55 ms (146
+// TFLOP/s, the library 7.20), dx 7.66, dW 8.30.  Bound by the matrix
+// instructions at the clock that they leave.  4096 tokens, 2048 -> 8192 with
+// SiLU and a checkpoint take 139 us, without the checkpoint 125, the bare
+// product 114: in the epilogues all workgroups write at once (100 MB) and none
+// multiplies.
 template <class T, int AM, int BM>
 __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int tj) {
   constexpr int kThreads = 512, BT = 256, NJ = 2;
@@ -856,7 +861,8 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(GemmArgs g, int ti, int
 // others multiply the last one's, and the two sums meet in LDS at the end.
 // (With 64 x 32 and every step for each wave the operands' reads took 768 cycles
 // of LDS a step, the matrix instructions 512: 74 us; with half of each step's k
-// 69.)  bf16, 2048 tokens, 8192 -> 2048: 69 us, 1.0 PFLOP/s; fp32 2048 cubed 132.
+// 69.)  bf16, 2048 tokens, 8192 -> 2048: 69 us, 1.0 PFLOP/s, the matrix
+// instructions busy 0.55 of the time; fp32 2048 cubed 129.
 template <class T, int AM, int BM>
 __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int tj) {
   constexpr int kThreads = 512, BT = 128;
@@ -960,7 +966,9 @@ __global__ __launch_bounds__(512) void gemm_mid_kernel(GemmArgs g, int ti, int t
     constexpr int kD = TA::kPer + (kCopyB ? TB::kPer : 0), kF = kCopyB ? 0 : TB::kLoads;
     // What every wave does in turn t: step t + 3's copies go to the buffer read
     // in turn t - 1, step t + 2's codes to that of turn t - 2.  Two steps' copies
-    // and codes may be under way when those of turn t + 1 have landed.
+    // and codes may be under way when those of turn t + 1 have landed.  (A run
+    // of codes is two loads and counts as one: the wait is then for some of turn
+    // t + 2's copies too.)
     auto feed = [&](int t, int slot, V* then, V* last) __attribute__((always_inline)) {
       copy(t + 3, last);
       put(slot, then);

@@ -135,7 +135,7 @@ int launch_few(FewArgs a, const void* W, int64_t ldw, hipStream_t stream) {
 }
 
 // Up to 16 tokens without a checkpoint.  (More are quicker in the products'
-// tiles: 32 tokens through 8192 x 8192 take 46 us there, 64 us here.)
+// tiles: 32 tokens through 8192 x 8192 take 42 to 46 us there, 64 us here.)
 int run_few(const FewArgs& a, const void* W, int64_t ldw, int dtype, hipStream_t stream) {
   return by_type(dtype, [&](auto t) -> int {
     using T = decltype(t);

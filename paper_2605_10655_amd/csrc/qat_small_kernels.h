@@ -162,7 +162,8 @@ struct SmallCodes : FewArgs {
 // and 7.3, 1024 x 1024 7.3 and 11.6.  Decoding into a dense matrix first takes
 // 6.1 and 6.1, 19.8 and 19.8; a table in LDS 33.8 and 34.0, 18.2 and 11.4.
 // With 12 state bits the table takes 4.7 for either at 1024 x 1024, this 5.1 and
-// 9.7.
+// 9.7.  (fp32, more than 4 tokens: 54 of the 16 tokens' registers lie in scratch;
+// 1024 x 1024 takes 20.2.)
 constexpr int kSmallUnit = 512;
 
 template <class T, int MT>

@@ -26,8 +26,8 @@ current stream or `stream`; outputs and workspaces come from PyTorch's
 allocator, from the pool of the stream that the call runs on, so that no two
 streams share a workspace and calls captured into a graph own theirs. On
 `stream` the inputs have to be ready, and live until it is done; what comes
-back may be used on the current stream once that has waited for `stream`. The
-autograd node is ``autograd.linear_act8``.
+back may be used on the current stream once that has waited for `stream`. No
+call here records a graph for autograd: that is ``autograd.linear_act8``.
 """
 from __future__ import annotations
 
@@ -260,7 +260,8 @@ def _new_act8(rows, cols, dtype, device):
 def act8_store(x, *, stream=None) -> Act8:
     """The 8-bit checkpoint of x [..., cols]: 1.0625 bytes a value, each at
     most half a step off, a step being at most 1/63.5 of its group's largest
-    magnitude."""
+    magnitude.  (Magnitudes past 65024 in float16, past 63.5 * 2^122 in the other
+    types, are less than a step off.)"""
     lib = _lib()
     m, ld = _matrix("x", x)
     dev = m.device
@@ -331,7 +332,9 @@ def linear_act_vjp(dy, x8, W, z8=None, activation="none", *, want_dx=True, want_
     """Backward pass of linear_act from the checkpoints x8 = act8_store(x) and
     z8: (dx [..., K], dW [N, K], dbias [N]), None where unwanted.  W is needed
     for dx only, x8 for dW only, z8 for an activation only; the residual's
-    gradient is dy."""
+    gradient is dy.  dz = dy * activation'(z) is rounded to the tensors' type, as
+    the products' operand (except in small layers); with float32 tensors it is
+    not."""
     lib = _lib()
     act = _activation(activation)
     d, ldd = _matrix("dy", dy)
@@ -475,7 +478,9 @@ def trellis_linear(x, packed, codebook, state_bits: int, k: int, V: int = 1, blo
     """y = activation(x W^T + bias) + residual for x [..., K] and W [N, K]
     given by its paths: packed [..., words] with N K / block paths, row n's
     blocks one after another, times scales (one a path) if given.  K must be a
-    multiple of block."""
+    multiple of block.  Weights are rounded to x's type, as the product's
+    operands, before or after their scale (of up to 16 tokens and few weights
+    they are not); with x in float32 they stay as they are."""
     lib = _lib()
     act = _activation(activation)
     m, ldx = _matrix("x", x)
