@@ -91,7 +91,7 @@ def _note_leaves(ctx, x):
     mark itself."""
     if not x.is_cuda:   # (linear_act refuses it)
         return
-    leaves = [n for n, _ in ctx.next_functions if n is not None and hasattr(n, "variable")]
+    leaves = [n for n, _ in ctx.next_functions if n is not None and n.name() == "torch::autograd::AccumulateGrad"]
     if not leaves:
         return
     if torch.cuda.is_current_stream_capturing():

@@ -877,6 +877,25 @@ def test_capture_is_refused_as_long_as_the_leafs_node_lives(monkeypatch):
     assert linear_act8(x, W) is not None and third is not None
 
 
+def test_only_leaves_count_for_a_capture(monkeypatch):
+    """Another operator's node is no leaf's, whatever it keeps."""
+    class Keeps(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, t):
+            ctx.variable = 1
+            return t.clone()
+
+        @staticmethod
+        def backward(ctx, g):
+            return g
+
+    x, W, _, _ = _padded_layer()
+    h = Keeps.apply(W.requires_grad_())
+    y = linear_act8(x, h)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    assert linear_act8(x, h) is not None and y is not None
+
+
 def test_no_gradient_keeps_no_checkpoint(monkeypatch):
     x, W, b, r = _padded_layer()
     W = W.requires_grad_()
